@@ -77,7 +77,9 @@ typedef enum cf_dev_flag {
     CF_FLAG_DOC_TOO_LONG = 4,   /* a document longer than the positional range                     */
     CF_FLAG_POS_OVERFLOW = 8,   /* an allocation that does not fit [pos_begin, pos_end)            */
     CF_FLAG_BAD_INDEX = 16,     /* candidate / ranked index outside [0, stride)                    */
-    CF_FLAG_POS_RANGE = 32      /* a segment or query whose stored or new positions leave [0, max_positions) */
+    CF_FLAG_POS_RANGE = 32,     /* a segment or query whose stored or new positions leave [0, max_positions) */
+    CF_FLAG_NONFINITE_VALUE = 64,/* NaN/Inf among the values handed to cf_quantize_cache                   */
+    CF_FLAG_NO_BLOCKS = 128     /* a request that cf_block_tables had no free blocks for                  */
 } cf_dev_flag;
 
 /* Geometry of one attention layer (host struct, passed by pointer, read during the call). */
@@ -375,6 +377,104 @@ CF_API cf_status cf_prefill_layer(const cf_layer_desc* desc,
                                   void* workspace, size_t workspace_bytes,
                                   const cf_prune_step* prune, int32_t n_pending, int32_t defer,
                                   int32_t* dev_flag, void* stream);
+
+/* =============================================================================================
+ * The Context KV Cache Store, and a decode cache, in 4 bits.
+ *
+ * Format.  A key or value row (token, kv head) of 128 channels is 64 bytes of codes and 4 scale bytes, 68 bytes instead of 256.
+ *   codes   channel c in byte c / 2, even channels in its lower four bits.  Bit 3 is the sign, bits 0-2 the index of a
+ *           magnitude in 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *   scales  byte g for channels 32g .. 32g + 31 stands for 2^(byte - 127); 255: every value of the group is NaN.
+ * (The e2m1 and e8m0 formats of the OCP microscaling specification, which the matrix unit of gfx950 reads directly.)  Every value
+ * that cf_quantize_cache writes is a number of the 16-bit type it was written from, so reading rounds nothing.
+ * Layout: the descriptor's store strides, in elements (channels): a row's codes lie at (t * store_token_stride + h *
+ * store_head_stride) / 2 bytes, its scales at a 32nd of that sum.  Both strides must be 0 or multiples of 128.
+ * The calls on such a store serve bf16 / fp16, head_dim 128, both pairings; others return CF_ERR_UNSUPPORTED. */
+typedef struct cf_q4_store {
+    void* k_codes;      /* device, 16-byte aligned */
+    void* k_scales;     /* device, 16-byte aligned */
+    void* v_codes;
+    void* v_scales;
+    int64_t n_tokens;   /* tokens the arrays hold  */
+} cf_q4_store;
+
+/* ---------------------------------------------------------------------------------------------
+ * Writes fresh keys and values to their slots of a 4-bit store.
+ *   k, v     device [n_tokens, n_kv_heads, 128] of desc->dtype, token-major
+ *   n_live   device int32 or NULL: rows at and past this number are padding and are not stored (the last entry of cf_block_tables' q_off,
+ *            for a call of fixed size in a graph)
+ *   slots    device int64 [n_tokens]: the store token that each goes to; negative: it is not stored.  Slots must be distinct (of a slot
+ *            named twice the contents are undefined).  One at or past store->n_tokens is not written and raises CF_FLAG_BAD_INDEX.
+ *   shift    device int32 [n_tokens] or NULL (0): positions by which the key is turned (Eq. 5) before it is rounded, so that a
+ *            key with local RoPE is cached at its position; one outside (-max_positions, max_positions) raises CF_FLAG_POS_RANGE
+ *            and its token is not written
+ * A group's scale is the smallest power of two with (largest magnitude) <= 7 * scale, its exponent at least -125 (bf16) / -23
+ * (fp16) and at most 125 / 13; values round to the nearest magnitude, ties to the even index, past 6 to 6.  The turn is
+ * computed in fp64 and rounded to fp32 ahead of that.  A group with a value that is not finite reads as NaN (CF_FLAG_NONFINITE_VALUE).
+ * Slots that are not named keep their contents. */
+CF_API cf_status cf_quantize_cache(const cf_layer_desc* desc, const void* k, const void* v, int32_t n_tokens, const int32_t* n_live,
+                                   const int64_t* slots, const int32_t* shift, const cf_q4_store* store, int32_t* dev_flag, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * cf_prefill_attention over a 4-bit store: the same mathematics, arguments and limits, with PREFIX and DOC entries read from `store`
+ * (NULL: no entry lists store tokens) and the own block in 16 bits.  Decode steps are calls with max_tq = 1.
+ * Stored keys and values enter as the numbers they stand for; the query, turned in fp32, enters with about 16 bits;
+ * probabilities are rounded to 11 bits or more, sums and partial rows are fp32.
+ * At most 256 table entries per query (CF_ERR_UNSUPPORTED beyond).  Own keys and values that are not finite reach only rows that see their
+ * token.
+ * The workspace (cf_prefill_workspace_bytes_q4, 256-byte aligned) holds scratch only; one for some max_kv_tokens and seg_stride
+ * serves every call of that batch and max_tq with smaller ones.  Calls that may overlap in time need workspaces of their own.
+ * Reductions run in a fixed order: the same inputs give bit-identical outputs, with masses asked for or not. */
+CF_API size_t cf_prefill_workspace_bytes_q4(const cf_layer_desc* desc, int32_t batch, int32_t max_tq, int32_t seg_stride,
+                                            int64_t max_kv_tokens);
+CF_API cf_status cf_prefill_attention_q4(const cf_layer_desc* desc, const void* q, const int32_t* q_off, int32_t q_stored_start,
+                                         const int32_t* q_new_start, const cf_q4_store* store, const void* k_self, const void* v_self,
+                                         const cf_segment* segs, const int32_t* n_seg, int32_t seg_stride, int32_t batch,
+                                         int32_t max_tq, int64_t max_kv_tokens, void* out, float* mass, float* score_accum,
+                                         int32_t score_stride, void* workspace, size_t workspace_bytes, int32_t* dev_flag,
+                                         void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * cf_assemble_cache out of a 4-bit store: the listed segments, moved to their final positions, as a contiguous 16-bit run.
+ * Same arguments; moved keys are rounded once to desc->dtype, unmoved keys and values are exact. */
+CF_API cf_status cf_assemble_cache_q4(const cf_layer_desc* desc, const cf_q4_store* store, const void* k_self, const void* v_self,
+                                      const int32_t* q_off, const cf_segment* segs, const int32_t* n_seg, int32_t seg_stride,
+                                      int32_t batch, int32_t max_tq, int32_t max_seg_len, const int64_t* final_off,
+                                      int64_t final_capacity, int64_t final_token_stride, int64_t final_head_stride, void* k_final,
+                                      void* v_final, int32_t* final_len, int32_t* final_pos, int32_t* dev_flag, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * One scheduler step of caches kept in blocks of `block_tokens` tokens that lie anywhere in a store: blocks are handed out and taken
+ * back, and what the step's calls take is written — slots and shifts (cf_quantize_cache), row offsets, positions and
+ * segment tables (cf_prefill_attention_q4, or cf_prefill_attention over a 16-bit store).  Once per step; every layer uses its tables.
+ *   cached     device int32 [batch]: tokens that each request holds, in ceil(cached / block_tokens) blocks
+ *   fresh      device int32 [batch]: tokens it adds in this step (0: none); negative: it leaves, its blocks go back
+ *   n_blocks   host: blocks of the pool; block i holds store tokens first_token + i * block_tokens ...
+ *   table      device int32 [batch*table_stride], in and out: the ids of a request's blocks, in order; new ones are appended.
+ *              table_stride <= 4095, batch <= 8192
+ *   free_blocks device int32 [n_blocks], in and out, and n_free, device int32 [1]: the free list, entries [0, n_free)
+ *   position   device int32 [batch] or NULL (0): position of a request's first cached token
+ *   base_segs, n_base, base_stride  device [batch*base_stride], [batch], or NULL: entries that lead each request's segment table
+ *              (shared prefix and documents)
+ *   q_stored_start  host: position that row 0 of a request's fresh q / k carries RoPE for
+ * Written:
+ *   next_len   [batch] tokens held after the step, next_n_free [1], the free list's length after it (neither may alias its input)
+ *   q_off      [batch+1], q_new_start [batch] = position + cached
+ *   slots      int64 [max_new_tokens], shift int32 [max_new_tokens]: of every fresh token, in request order; the rest is not touched
+ *   segs       [batch*seg_stride], n_seg [batch]: base entries, the cached tokens (neighbouring blocks as one entry; kind PREFIX) and, with
+ *              fresh tokens, the own block.  A request that leaves has none.
+ * Order: blocks of leaving requests go on top of the free list, by request and place; then the others take theirs off the top, by
+ * request and place.  A request is served if it needs no block or the needs up to and with its own fit; one that is not keeps
+ * its cached tokens, its fresh ones get slot -1 and next_len does not count them (CF_FLAG_NO_BLOCKS), though its rows still attend.
+ * A request whose lengths do not fit its table is not served either (CF_FLAG_BAD_INDEX; with more cached tokens than the table
+ * holds, or a negative number, its table is empty too), and bad block ids give slots of -1 and empty entries (CF_FLAG_BAD_INDEX).
+ * More entries than seg_stride: n_seg = 0 and CF_FLAG_BAD_SEGMENT.  Fresh tokens past max_new_tokens: not written, CF_FLAG_BAD_INDEX. */
+CF_API cf_status cf_block_tables(const int32_t* cached, const int32_t* fresh, int32_t batch, int32_t block_tokens, int32_t n_blocks,
+                                 int64_t first_token, int32_t* table, int32_t table_stride, int32_t* free_blocks,
+                                 const int32_t* n_free, const int32_t* position, const cf_segment* base_segs, const int32_t* n_base,
+                                 int32_t base_stride, int32_t q_stored_start, int32_t* next_len, int32_t* next_n_free, int32_t* q_off,
+                                 int32_t* q_new_start, int64_t* slots, int32_t* shift, int64_t max_new_tokens, cf_segment* segs,
+                                 int32_t* n_seg, int32_t seg_stride, int32_t* dev_flag, void* stream);
 
 /* Thread-local text for the last non-OK status returned on this thread (static storage). */
 CF_API const char* cf_last_error(void);

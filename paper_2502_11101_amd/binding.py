@@ -25,13 +25,14 @@ CF_ROPE_HALF, CF_ROPE_INTERLEAVED = 0, 1
 CF_SEG_PREFIX, CF_SEG_DOC, CF_SEG_SELF = 0, 1, 2
 CF_ALLOC_KEEP, CF_ALLOC_ALIGN, CF_ALLOC_SORT = 0, 1, 2
 CF_FLAG_BAD_SEGMENT, CF_FLAG_NONFINITE_SCORE, CF_FLAG_DOC_TOO_LONG, CF_FLAG_POS_OVERFLOW, CF_FLAG_BAD_INDEX = 1, 2, 4, 8, 16
-CF_FLAG_POS_RANGE = 32
+CF_FLAG_POS_RANGE, CF_FLAG_NONFINITE_VALUE, CF_FLAG_NO_BLOCKS = 32, 64, 128
 
 DTYPE_CODE = {"f32": CF_F32, "bf16": CF_BF16, "f16": CF_F16}
 
 EXPORTS = ("cf_reposition_keys", "cf_prefill_workspace_bytes", "cf_prefill_attention", "cf_prune_topk",
            "cf_assign_positions", "cf_gather_segments", "cf_last_error", "cf_version", "cf_calibrate", "cf_profile_kernel_events", "cf_profile_kernel_ms",
-           "cf_prefill_layer", "cf_assemble_cache", "cf_prefill_attention_static")
+           "cf_prefill_layer", "cf_assemble_cache", "cf_prefill_attention_static", "cf_quantize_cache", "cf_prefill_workspace_bytes_q4",
+           "cf_prefill_attention_q4", "cf_assemble_cache_q4", "cf_block_tables")
 CF_STATIC_SCRATCH_BYTES = 32 << 20
 CF_MAX_PENDING = 15
 
@@ -51,6 +52,11 @@ class cf_prune_step(C.Structure):
                 ("doc_tok_offset", C.c_void_p), ("doc_len", C.c_void_p), ("cand", C.c_void_p), ("n_cand", C.c_void_p),
                 ("keep_idx", C.c_void_p), ("n_keep", C.c_void_p), ("new_start", C.c_void_p), ("q_start", C.c_void_p),
                 ("n_reuse", C.c_void_p), ("order", C.c_void_p), ("next_segs", C.c_void_p), ("next_n_seg", C.c_void_p)]
+
+
+class cf_q4_store(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+                ("n_tokens", C.c_int64)]
 
 
 SEGMENT_DTYPE = np.dtype([("tok_offset", "<i8"), ("len", "<i4"), ("stored_start", "<i4"),
@@ -121,6 +127,18 @@ def load() -> C.CDLL:
                                       vp, vp, vp]
     lib.cf_gather_segments.restype = i32
     lib.cf_gather_segments.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp]
+    sp = C.POINTER(cf_q4_store)
+    lib.cf_quantize_cache.restype = i32
+    lib.cf_quantize_cache.argtypes = [dp, vp, vp, i32, vp, vp, vp, sp, vp, vp]
+    lib.cf_prefill_workspace_bytes_q4.restype = sz
+    lib.cf_prefill_workspace_bytes_q4.argtypes = [dp, i32, i32, i32, i64]
+    lib.cf_prefill_attention_q4.restype = i32
+    lib.cf_prefill_attention_q4.argtypes = [dp, vp, vp, i32, vp, sp, vp, vp, vp, vp, i32, i32, i32, i64, vp, vp, vp, i32, vp, sz, vp, vp]
+    lib.cf_assemble_cache_q4.restype = i32
+    lib.cf_assemble_cache_q4.argtypes = [dp, sp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp]
+    lib.cf_block_tables.restype = i32
+    lib.cf_block_tables.argtypes = [vp, vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp, vp,
+                                    i32, vp, vp]
     _lib = lib
     return lib
 
@@ -300,5 +318,52 @@ def cf_gather_segments(doc_tok_offset, len_, order, n_order, new_start, q_start,
     status = (_native or _call()).gather_segments(
         doc_tok_offset, len_, order, n_order, new_start, q_start, q_off, batch, stride, prefix_len, doc_stored_start,
         q_stored_start, segs, n_seg, seg_stride, dev_flag, stream)
+    if status:
+        _check(status)
+
+
+def make_q4_store(k_codes, k_scales, v_codes, v_scales, n_tokens: int) -> cf_q4_store:
+    """A cache store in 4 bits: codes [.., 64] and scale bytes [.., 4] of keys and values, uint8, laid out by the descriptor's strides.
+    The structure holds addresses: keep the tensors as long as it is used."""
+    return cf_q4_store(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), int(n_tokens))
+
+
+def cf_quantize_cache(desc, k, v, n_tokens: int, slots, shift, store: cf_q4_store, dev_flag=None, stream=None, n_live=None) -> None:
+    status = (_native or _call()).quantize_cache(desc, k, v, n_tokens, n_live, slots, shift, store, dev_flag, stream)
+    if status:
+        _check(status)
+
+
+def cf_prefill_workspace_bytes_q4(desc, batch: int, max_tq: int, seg_stride: int, max_kv_tokens: int) -> int:
+    return int(load().cf_prefill_workspace_bytes_q4(C.byref(desc), batch, max_tq, seg_stride, max_kv_tokens))
+
+
+def cf_prefill_attention_q4(desc, q, q_off, q_stored_start: int, q_new_start, store: Optional[cf_q4_store], k_self, v_self, segs, n_seg,
+                            seg_stride: int, batch: int, max_tq: int, max_kv_tokens: int, out, mass, score_accum, score_stride: int,
+                            workspace, workspace_bytes: int, dev_flag=None, stream=None) -> None:
+    status = (_native or _call()).prefill_attention_q4(
+        desc, q, q_off, q_stored_start, q_new_start, store, k_self, v_self, segs, n_seg, seg_stride, batch, max_tq, max_kv_tokens, out,
+        mass, score_accum, score_stride, workspace, workspace_bytes, dev_flag, stream)
+    if status:
+        _check(status)
+
+
+def cf_assemble_cache_q4(desc, store: cf_q4_store, k_self, v_self, q_off, segs, n_seg, seg_stride: int, batch: int, max_tq: int,
+                         max_seg_len: int, final_off, final_capacity: int, final_token_stride: int, final_head_stride: int, k_final,
+                         v_final, final_len, final_pos=None, dev_flag=None, stream=None) -> None:
+    status = (_native or _call()).assemble_cache_q4(
+        desc, store, k_self, v_self, q_off, segs, n_seg, seg_stride, batch, max_tq, max_seg_len, final_off, final_capacity,
+        final_token_stride, final_head_stride, k_final, v_final, final_len, final_pos, dev_flag, stream)
+    if status:
+        _check(status)
+
+
+def cf_block_tables(cached, fresh, batch: int, block_tokens: int, n_blocks: int, first_token: int, table, table_stride: int, free_blocks,
+                    n_free, position, base_segs, n_base, base_stride: int, q_stored_start: int, next_len, next_n_free, q_off, q_new_start,
+                    slots, shift, max_new_tokens: int, segs, n_seg, seg_stride: int, dev_flag=None, stream=None) -> None:
+    status = (_native or _call()).block_tables(
+        cached, fresh, batch, block_tokens, n_blocks, first_token, table, table_stride, free_blocks, n_free, position, base_segs, n_base,
+        base_stride, q_stored_start, next_len, next_n_free, q_off, q_new_start, slots, shift, max_new_tokens, segs, n_seg, seg_stride,
+        dev_flag, stream)
     if status:
         _check(status)

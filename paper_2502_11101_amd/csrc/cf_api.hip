@@ -69,6 +69,17 @@ cf_status check_desc(const cf_layer_desc* d) {
     return CF_OK;
 }
 
+// What the calls on a store in 4 bits take of a descriptor.
+static cf_status check_desc_q4(const cf_layer_desc* d) {
+    cf_status st = check_desc(d);
+    if (st != CF_OK) return st;
+    CF_REQUIRE((d->dtype == CF_BF16 || d->dtype == CF_F16) && d->head_dim == 128, CF_ERR_UNSUPPORTED,
+               "a store in 4 bits serves bf16 and fp16 with head_dim 128");
+    CF_REQUIRE(d->store_token_stride % 128 == 0 && d->store_head_stride % 128 == 0, CF_ERR_INVALID_ARG,
+               "the strides of a store in 4 bits must be multiples of 128 elements");
+    return CF_OK;
+}
+
 // A thread keeps the table of the model it called with last: 64 powers are 2-3 us, a third of the host's time for a call.
 const RopeFreq& rope_freq(const cf_layer_desc* d) {
     thread_local RopeFreq f;
@@ -86,6 +97,15 @@ const RopeFreq& rope_freq(const cf_layer_desc* d) {
 }
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+static cf_status check_q4_store(const cf_q4_store* st) {
+    CF_REQUIRE(st->n_tokens >= 0, CF_ERR_INVALID_ARG, "store: negative token count");
+    CF_REQUIRE(st->n_tokens == 0 || (st->k_codes && st->k_scales && st->v_codes && st->v_scales), CF_ERR_INVALID_ARG,
+               "store: NULL array but n_tokens > 0");
+    CF_REQUIRE(aligned16(st->k_codes) && aligned16(st->k_scales) && aligned16(st->v_codes) && aligned16(st->v_scales),
+               CF_ERR_INVALID_ARG, "store: arrays must be 16-byte aligned");
+    return CF_OK;
+}
 
 cf_status launch_prune_step(const AttnArgs& a, const cf_prune_step* pr, hipStream_t s) {
     cf_status st = launch_prune(a.score_accum, pr->normalise_by_len ? pr->doc_len : nullptr, pr->cand, pr->n_cand, pr->keep,
@@ -207,28 +227,25 @@ static cf_status check_prune_step(const cf_prune_step* pr, int32_t seg_stride, c
     return CF_OK;
 }
 
-static cf_status prefill_impl(const cf_layer_desc* desc, const void* q, const int32_t* q_off,
-                               int32_t q_stored_start, const int32_t* q_new_start, const void* k_store,
-                               const void* v_store, int64_t n_store_tokens, const void* k_self,
-                               const void* v_self, const cf_segment* segs, const int32_t* n_seg,
-                               int32_t seg_stride, int32_t batch, int32_t max_tq, int64_t max_kv_tokens,
-                               void* out, float* mass, float* score_accum, int32_t score_stride,
-                               void* workspace, size_t workspace_bytes, const cf_prune_step* prune,
-                               int32_t n_pending, int32_t defer, int32_t* dev_flag, void* stream, bool row_by_row = false) {
-    cf_status st = check_desc(desc);
-    if (st != CF_OK) return st;
-    CF_REQUIRE(batch >= 0, CF_ERR_INVALID_ARG, "batch is negative");
-    CF_REQUIRE(n_pending >= 0 && n_pending <= kMaxPending && (defer == 0 || defer == 1), CF_ERR_INVALID_ARG,
-               "n_pending must be in [0, %d] and defer 0 or 1", kMaxPending);
-    CF_REQUIRE(!(defer && prune), CF_ERR_INVALID_ARG, "a call with a prune step cannot defer its scores");
-    CF_REQUIRE(!(defer && n_pending == kMaxPending), CF_ERR_INVALID_ARG, "%d layers are pending already: flush first", kMaxPending);
+}  // extern "C"
+
+// Checks the arguments that every attention call takes and fills `*args` with them; *run: whether there is anything to do.
+// need(false): the bytes of workspace that the call needs; need(true): those reported for its sizes.
+template <class F>
+static cf_status attention_args(const cf_layer_desc* desc, const void* q, const int32_t* q_off, int32_t q_stored_start,
+                                const int32_t* q_new_start, const void* k_store, const void* v_store, int64_t n_store_tokens,
+                                const void* k_self, const void* v_self, const cf_segment* segs, const int32_t* n_seg, int32_t seg_stride,
+                                int32_t batch, int32_t max_tq, int64_t max_kv_tokens, void* out, float* mass, float* score_accum,
+                                int32_t score_stride, void* workspace, size_t workspace_bytes, const cf_prune_step* prune, F need,
+                                int32_t* dev_flag, AttnArgs* args, bool* run) {
+    *run = false;
     CF_REQUIRE(max_tq >= 1, CF_ERR_INVALID_ARG, "max_tq must be >= 1");
     CF_REQUIRE(seg_stride >= 1, CF_ERR_INVALID_ARG, "seg_stride must be >= 1");
     CF_REQUIRE(n_store_tokens >= 0 && max_kv_tokens >= 0, CF_ERR_INVALID_ARG, "negative token count");
     CF_REQUIRE(score_accum == nullptr || score_stride >= 1, CF_ERR_INVALID_ARG,
                "score_stride must be >= 1 when score_accum is given");
     if (prune) {
-        st = check_prune_step(prune, seg_stride, score_accum, score_stride, segs, n_seg, q_new_start);
+        const cf_status st = check_prune_step(prune, seg_stride, score_accum, score_stride, segs, n_seg, q_new_start);
         if (st != CF_OK) return st;
     }
     if (batch == 0) return CF_OK;
@@ -245,15 +262,12 @@ static cf_status prefill_impl(const cf_layer_desc* desc, const void* q, const in
                CF_ERR_INVALID_ARG, "tensor base pointers must be 16-byte aligned");
     CF_REQUIRE(q_stored_start >= 0 && q_stored_start < desc->max_positions, CF_ERR_RANGE,
                "q_stored_start outside [0, max_positions)");
-    const size_t need = row_by_row ? generic_workspace_bytes(desc, batch, max_tq, seg_stride)
-                                   : call_bytes(desc, batch, max_tq, seg_stride, max_kv_tokens, workspace_bytes);
-    CF_REQUIRE(workspace != nullptr && workspace_bytes >= need, CF_ERR_WORKSPACE,
-               "workspace too small: %zu bytes given, %zu needed", workspace_bytes,
-               row_by_row ? need : cf_prefill_workspace_bytes(desc, batch, max_tq, seg_stride, max_kv_tokens));
+    CF_REQUIRE(workspace != nullptr && workspace_bytes >= need(false), CF_ERR_WORKSPACE,
+               "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need(true));
     CF_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, CF_ERR_WORKSPACE,
                "workspace must be 256-byte aligned");
 
-    AttnArgs a;
+    AttnArgs& a = *args;
     std::memset(&a, 0, sizeof(a));
     a.q = q; a.q_off = q_off; a.q_stored_start = q_stored_start; a.q_new_start = q_new_start;
     a.k_store = k_store; a.v_store = v_store; a.n_store_tokens = n_store_tokens;
@@ -268,6 +282,38 @@ static cf_status prefill_impl(const cf_layer_desc* desc, const void* q, const in
     a.store_ts = store_token_stride(desc);
     a.store_hs = store_head_stride(desc);
     a.max_positions = desc->max_positions;
+    *run = true;
+    return CF_OK;
+}
+
+extern "C" {
+
+static cf_status prefill_impl(const cf_layer_desc* desc, const void* q, const int32_t* q_off,
+                               int32_t q_stored_start, const int32_t* q_new_start, const void* k_store,
+                               const void* v_store, int64_t n_store_tokens, const void* k_self,
+                               const void* v_self, const cf_segment* segs, const int32_t* n_seg,
+                               int32_t seg_stride, int32_t batch, int32_t max_tq, int64_t max_kv_tokens,
+                               void* out, float* mass, float* score_accum, int32_t score_stride,
+                               void* workspace, size_t workspace_bytes, const cf_prune_step* prune,
+                               int32_t n_pending, int32_t defer, int32_t* dev_flag, void* stream, bool row_by_row = false) {
+    cf_status st = check_desc(desc);
+    if (st != CF_OK) return st;
+    CF_REQUIRE(batch >= 0, CF_ERR_INVALID_ARG, "batch is negative");
+    CF_REQUIRE(n_pending >= 0 && n_pending <= kMaxPending && (defer == 0 || defer == 1), CF_ERR_INVALID_ARG,
+               "n_pending must be in [0, %d] and defer 0 or 1", kMaxPending);
+    CF_REQUIRE(!(defer && prune), CF_ERR_INVALID_ARG, "a call with a prune step cannot defer its scores");
+    CF_REQUIRE(!(defer && n_pending == kMaxPending), CF_ERR_INVALID_ARG, "%d layers are pending already: flush first", kMaxPending);
+    const auto need = [&](bool reported) {
+        return row_by_row ? generic_workspace_bytes(desc, batch, max_tq, seg_stride)
+               : reported ? cf_prefill_workspace_bytes(desc, batch, max_tq, seg_stride, max_kv_tokens)
+                          : call_bytes(desc, batch, max_tq, seg_stride, max_kv_tokens, workspace_bytes);
+    };
+    AttnArgs a;
+    bool run = false;
+    st = attention_args(desc, q, q_off, q_stored_start, q_new_start, k_store, v_store, n_store_tokens, k_self, v_self, segs, n_seg, seg_stride,
+                        batch, max_tq, max_kv_tokens, out, mass, score_accum, score_stride, workspace, workspace_bytes, prune, need, dev_flag,
+                        &a, &run);
+    if (st != CF_OK || !run) return st;
     a.n_pending = n_pending;
     a.defer = defer;
     const RopeFreq& f = rope_freq(desc);
@@ -417,14 +463,12 @@ cf_status cf_gather_segments(const int64_t* doc_tok_offset, const int32_t* len, 
                          static_cast<hipStream_t>(stream));
 }
 
-cf_status cf_assemble_cache(const cf_layer_desc* desc, const void* k_store, const void* v_store, int64_t n_store_tokens,
-                            const void* k_self, const void* v_self, const int32_t* q_off, const cf_segment* segs,
-                            const int32_t* n_seg, int32_t seg_stride, int32_t batch, int32_t max_tq, int32_t max_seg_len,
-                            const int64_t* final_off, int64_t final_capacity, int64_t final_token_stride,
-                            int64_t final_head_stride, void* k_final, void* v_final, int32_t* final_len,
-                            int32_t* final_pos, int32_t* dev_flag, void* stream) {
-    cf_status st = check_desc(desc);
-    if (st != CF_OK) return st;
+static cf_status assemble_impl(const cf_layer_desc* desc, const void* k_store, const void* v_store, const uint8_t* k_scales,
+                               const uint8_t* v_scales, int64_t n_store_tokens, const void* k_self, const void* v_self,
+                               const int32_t* q_off, const cf_segment* segs, const int32_t* n_seg, int32_t seg_stride, int32_t batch,
+                               int32_t max_tq, int32_t max_seg_len, const int64_t* final_off, int64_t final_capacity,
+                               int64_t final_token_stride, int64_t final_head_stride, void* k_final, void* v_final,
+                               int32_t* final_len, int32_t* final_pos, int32_t* dev_flag, void* stream) {
     CF_REQUIRE(batch >= 0, CF_ERR_INVALID_ARG, "batch is negative");
     CF_REQUIRE(seg_stride >= 1 && max_tq >= 1 && max_seg_len >= 1, CF_ERR_INVALID_ARG,
                "seg_stride, max_tq and max_seg_len must be >= 1");
@@ -446,7 +490,8 @@ cf_status cf_assemble_cache(const cf_layer_desc* desc, const void* k_store, cons
                CF_ERR_INVALID_ARG, "k_final / v_final must not alias the inputs or each other");
     AssembleArgs a;
     std::memset(&a, 0, sizeof(a));
-    a.k_store = k_store; a.v_store = v_store; a.k_self = k_self; a.v_self = v_self; a.k_final = k_final; a.v_final = v_final;
+    a.k_store = k_store; a.v_store = v_store; a.k_scales = k_scales; a.v_scales = v_scales; a.k_self = k_self; a.v_self = v_self;
+    a.k_final = k_final; a.v_final = v_final;
     a.q_off = q_off; a.segs = segs; a.n_seg = n_seg; a.final_off = final_off; a.final_len = final_len; a.final_pos = final_pos;
     a.dev_flag = dev_flag; a.n_store_tokens = n_store_tokens; a.final_capacity = final_capacity;
     a.store_ts = store_token_stride(desc); a.store_hs = store_head_stride(desc);
@@ -455,6 +500,122 @@ cf_status cf_assemble_cache(const cf_layer_desc* desc, const void* k_store, cons
     a.max_positions = desc->max_positions;
     const RopeFreq& f = rope_freq(desc);
     return launch_assemble(desc, f, a, max_seg_len, static_cast<hipStream_t>(stream));
+}
+
+cf_status cf_assemble_cache(const cf_layer_desc* desc, const void* k_store, const void* v_store, int64_t n_store_tokens,
+                            const void* k_self, const void* v_self, const int32_t* q_off, const cf_segment* segs,
+                            const int32_t* n_seg, int32_t seg_stride, int32_t batch, int32_t max_tq, int32_t max_seg_len,
+                            const int64_t* final_off, int64_t final_capacity, int64_t final_token_stride,
+                            int64_t final_head_stride, void* k_final, void* v_final, int32_t* final_len,
+                            int32_t* final_pos, int32_t* dev_flag, void* stream) {
+    cf_status st = check_desc(desc);
+    if (st != CF_OK) return st;
+    return assemble_impl(desc, k_store, v_store, nullptr, nullptr, n_store_tokens, k_self, v_self, q_off, segs, n_seg, seg_stride, batch,
+                         max_tq, max_seg_len, final_off, final_capacity, final_token_stride, final_head_stride, k_final, v_final,
+                         final_len, final_pos, dev_flag, stream);
+}
+
+cf_status cf_assemble_cache_q4(const cf_layer_desc* desc, const cf_q4_store* store, const void* k_self, const void* v_self,
+                               const int32_t* q_off, const cf_segment* segs, const int32_t* n_seg, int32_t seg_stride, int32_t batch,
+                               int32_t max_tq, int32_t max_seg_len, const int64_t* final_off, int64_t final_capacity,
+                               int64_t final_token_stride, int64_t final_head_stride, void* k_final, void* v_final,
+                               int32_t* final_len, int32_t* final_pos, int32_t* dev_flag, void* stream) {
+    cf_status st = check_desc_q4(desc);
+    if (st != CF_OK) return st;
+    CF_REQUIRE(store != nullptr, CF_ERR_INVALID_ARG, "store is NULL");
+    st = check_q4_store(store);
+    if (st != CF_OK) return st;
+    // without store tokens nothing is read as 4 bits: the entries that are left are own blocks
+    const bool any = store->n_tokens > 0;
+    return assemble_impl(desc, any ? store->k_codes : nullptr, any ? store->v_codes : nullptr,
+                         any ? static_cast<const uint8_t*>(store->k_scales) : nullptr,
+                         any ? static_cast<const uint8_t*>(store->v_scales) : nullptr, store->n_tokens, k_self, v_self, q_off, segs, n_seg,
+                         seg_stride, batch, max_tq, max_seg_len, final_off, final_capacity, final_token_stride, final_head_stride,
+                         k_final, v_final, final_len, final_pos, dev_flag, stream);
+}
+
+cf_status cf_quantize_cache(const cf_layer_desc* desc, const void* k, const void* v, int32_t n_tokens, const int32_t* n_live,
+                            const int64_t* slots, const int32_t* shift, const cf_q4_store* store, int32_t* dev_flag, void* stream) {
+    cf_status st = check_desc_q4(desc);
+    if (st != CF_OK) return st;
+    CF_REQUIRE(n_tokens >= 0, CF_ERR_INVALID_ARG, "n_tokens is negative");
+    CF_REQUIRE(store != nullptr, CF_ERR_INVALID_ARG, "store is NULL");
+    st = check_q4_store(store);
+    if (st != CF_OK) return st;
+    if (n_tokens == 0) return CF_OK;
+    CF_REQUIRE(k && v && slots, CF_ERR_INVALID_ARG, "k, v and slots must not be NULL");
+    CF_REQUIRE(aligned16(k) && aligned16(v), CF_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+    QuantizeArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.k = k; a.v = v; a.n_live = n_live; a.slots = slots; a.shift = shift;
+    a.k_codes = static_cast<uint8_t*>(store->k_codes); a.k_scales = static_cast<uint8_t*>(store->k_scales);
+    a.v_codes = static_cast<uint8_t*>(store->v_codes); a.v_scales = static_cast<uint8_t*>(store->v_scales);
+    a.n_store_tokens = store->n_tokens; a.store_ts = store_token_stride(desc); a.store_hs = store_head_stride(desc);
+    a.dev_flag = dev_flag; a.n_tokens = n_tokens; a.n_kv_heads = desc->n_kv_heads; a.max_positions = desc->max_positions;
+    return launch_quantize(desc, rope_freq(desc), a, static_cast<hipStream_t>(stream));
+}
+
+size_t cf_prefill_workspace_bytes_q4(const cf_layer_desc* desc, int32_t batch, int32_t max_tq, int32_t seg_stride, int64_t max_kv_tokens) {
+    if (check_desc_q4(desc) != CF_OK) return 0;
+    if (batch <= 0 || max_tq <= 0 || seg_stride <= 0 || seg_stride > kMaxQ4Entries || max_kv_tokens < 0) return 0;
+    return q4_workspace_bytes(desc, batch, max_tq, seg_stride, max_kv_tokens);
+}
+
+cf_status cf_prefill_attention_q4(const cf_layer_desc* desc, const void* q, const int32_t* q_off, int32_t q_stored_start,
+                                  const int32_t* q_new_start, const cf_q4_store* store, const void* k_self, const void* v_self,
+                                  const cf_segment* segs, const int32_t* n_seg, int32_t seg_stride, int32_t batch, int32_t max_tq,
+                                  int64_t max_kv_tokens, void* out, float* mass, float* score_accum, int32_t score_stride,
+                                  void* workspace, size_t workspace_bytes, int32_t* dev_flag, void* stream) {
+    cf_status st = check_desc_q4(desc);
+    if (st != CF_OK) return st;
+    static const cf_q4_store none = {};
+    const cf_q4_store& from = store ? *store : none;
+    st = check_q4_store(&from);
+    if (st != CF_OK) return st;
+    CF_REQUIRE(seg_stride <= kMaxQ4Entries, CF_ERR_UNSUPPORTED, "more than %d table entries per query", kMaxQ4Entries);
+    AttnArgs a;
+    bool run = false;
+    CF_REQUIRE(batch >= 0, CF_ERR_INVALID_ARG, "batch is negative");
+    const auto need = [&](bool) { return q4_workspace_bytes(desc, batch, max_tq, seg_stride, max_kv_tokens); };
+    st = attention_args(desc, q, q_off, q_stored_start, q_new_start, from.k_codes, from.v_codes, from.n_tokens, k_self, v_self, segs, n_seg,
+                        seg_stride, batch, max_tq, max_kv_tokens, out, mass, score_accum, score_stride, workspace, workspace_bytes, nullptr,
+                        need, dev_flag, &a, &run);
+    if (st != CF_OK || !run) return st;
+    const q4::Scales sc = {static_cast<const uint8_t*>(from.k_scales), static_cast<const uint8_t*>(from.v_scales)};
+    return launch_attention_q4(a, sc, rope_freq(desc), static_cast<hipStream_t>(stream));
+}
+
+cf_status cf_block_tables(const int32_t* cached, const int32_t* fresh, int32_t batch, int32_t block_tokens, int32_t n_blocks,
+                          int64_t first_token, int32_t* table, int32_t table_stride, int32_t* free_blocks, const int32_t* n_free,
+                          const int32_t* position, const cf_segment* base_segs, const int32_t* n_base, int32_t base_stride,
+                          int32_t q_stored_start, int32_t* next_len, int32_t* next_n_free, int32_t* q_off, int32_t* q_new_start,
+                          int64_t* slots, int32_t* shift, int64_t max_new_tokens, cf_segment* segs, int32_t* n_seg, int32_t seg_stride,
+                          int32_t* dev_flag, void* stream) {
+    CF_REQUIRE(batch >= 0, CF_ERR_INVALID_ARG, "batch is negative");
+    CF_REQUIRE(batch <= kMaxBlockBatch, CF_ERR_UNSUPPORTED, "more than %d requests", kMaxBlockBatch);
+    CF_REQUIRE(block_tokens >= 1 && n_blocks >= 0 && first_token >= 0, CF_ERR_INVALID_ARG,
+               "need block_tokens >= 1, n_blocks >= 0 and first_token >= 0");
+    CF_REQUIRE(table_stride >= 1 && seg_stride >= 1 && max_new_tokens >= 0, CF_ERR_INVALID_ARG,
+               "need table_stride >= 1, seg_stride >= 1 and max_new_tokens >= 0");
+    CF_REQUIRE(table_stride <= kMaxBlockTable, CF_ERR_UNSUPPORTED, "more than %d blocks per request", kMaxBlockTable);
+    CF_REQUIRE(q_stored_start >= 0, CF_ERR_RANGE, "q_stored_start is negative");
+    CF_REQUIRE((base_segs == nullptr) == (n_base == nullptr) && (base_segs == nullptr || base_stride >= 1), CF_ERR_INVALID_ARG,
+               "base_segs and n_base must be given together, with base_stride >= 1");
+    if (batch == 0) return CF_OK;
+    CF_REQUIRE(cached && fresh && table && (free_blocks || n_blocks == 0) && n_free && next_len && next_n_free && q_off && q_new_start &&
+                   segs && n_seg,
+               CF_ERR_INVALID_ARG, "NULL table pointer");
+    CF_REQUIRE(max_new_tokens == 0 || (slots && shift), CF_ERR_INVALID_ARG, "slots and shift must not be NULL");
+    CF_REQUIRE(next_len != cached && next_len != fresh && next_n_free != n_free && segs != base_segs, CF_ERR_INVALID_ARG,
+               "next_len, next_n_free and segs must not alias cached, fresh, n_free and base_segs");
+    BlockArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.cached = cached; a.fresh = fresh; a.n_free = n_free; a.position = position; a.base_segs = base_segs; a.n_base = n_base;
+    a.table = table; a.free_blocks = free_blocks; a.next_len = next_len; a.next_n_free = next_n_free; a.q_off = q_off;
+    a.q_new_start = q_new_start; a.shift = shift; a.n_seg = n_seg; a.dev_flag = dev_flag; a.slots = slots; a.segs = segs;
+    a.first_token = first_token; a.max_new_tokens = max_new_tokens; a.batch = batch; a.block_tokens = block_tokens; a.n_blocks = n_blocks;
+    a.table_stride = table_stride; a.base_stride = base_stride; a.q_stored_start = q_stored_start; a.seg_stride = seg_stride;
+    return launch_block_tables(a, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

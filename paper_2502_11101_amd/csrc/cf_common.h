@@ -147,6 +147,7 @@ __device__ __forceinline__ float wave_sum_dpp(float v) {
 // ---------------------------------------------------------------------------------- launchers
 struct AssembleArgs {
     const void *k_store, *v_store, *k_self, *v_self;
+    const uint8_t *k_scales, *v_scales;      // of a store in 4 bits (k_store, v_store are its codes), else NULL
     void *k_final, *v_final;
     const int32_t* q_off;
     const cf_segment* segs;
@@ -158,6 +159,29 @@ struct AssembleArgs {
 };
 cf_status launch_assemble(const cf_layer_desc* d, const RopeFreq& f, const AssembleArgs& a, int32_t max_seg_len,
                           hipStream_t s);
+
+struct QuantizeArgs {
+    const void *k, *v;
+    const int64_t* slots;
+    const int32_t *shift, *n_live;
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int64_t n_store_tokens, store_ts, store_hs;
+    int32_t* dev_flag;
+    int32_t n_tokens, n_kv_heads, max_positions, e_lo, e_hi;
+};
+cf_status launch_quantize(const cf_layer_desc* d, const RopeFreq& f, QuantizeArgs a, hipStream_t s);
+
+struct BlockArgs {
+    const int32_t *cached, *fresh, *n_free, *position, *n_base;
+    const cf_segment* base_segs;
+    int32_t *table, *free_blocks, *next_len, *next_n_free, *q_off, *q_new_start, *shift, *n_seg, *dev_flag;
+    int64_t* slots;
+    cf_segment* segs;
+    int64_t first_token, max_new_tokens;
+    int32_t batch, block_tokens, n_blocks, table_stride, base_stride, q_stored_start, seg_stride;
+};
+constexpr int kMaxBlockBatch = 8192, kMaxBlockTable = 4095;      // what the kernel's LDS holds
+cf_status launch_block_tables(const BlockArgs& a, hipStream_t s);
 
 cf_status launch_reposition(const cf_layer_desc* d, const RopeFreq& f, const void* k_in, void* k_out,
                             const cf_segment* segs, int32_t n_seg, int64_t n_store_tokens,
@@ -216,6 +240,13 @@ size_t mfma_workspace_bytes(const cf_layer_desc* d, int32_t batch, int32_t max_t
                             int64_t max_kv_tokens);
 size_t mfma_call_bytes(const cf_layer_desc* d, int32_t batch, int32_t max_tq, int32_t seg_stride, int64_t max_kv_tokens, size_t given);
 cf_status launch_attention_mfma(const AttnArgs& a, const RopeFreq& f, hipStream_t s, const cf_prune_step* prune);
+// the attention over a store in 4 bits (a.k_store, a.v_store: its codes)
+namespace q4 {
+struct Scales { const uint8_t *k, *v; };
+}
+constexpr int kMaxQ4Entries = 256;           // table entries of a query
+size_t q4_workspace_bytes(const cf_layer_desc* d, int32_t batch, int32_t max_tq, int32_t seg_stride, int64_t max_kv_tokens);
+cf_status launch_attention_q4(const AttnArgs& a, const q4::Scales& sc, const RopeFreq& f, hipStream_t s);
 // the three stand-alone launches of a prune step (ranking, allocation, table rebuild)
 cf_status launch_prune_step(const AttnArgs& a, const cf_prune_step* prune, hipStream_t s);
 

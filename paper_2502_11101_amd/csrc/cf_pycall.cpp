@@ -179,6 +179,62 @@ CF_PY(assemble_cache) {
     });
 }
 
+CF_PY(prefill_attention_q4) {
+    Args a(args, nargs, 22, "prefill_attention_q4");
+    const cf_layer_desc* desc = a.structure<cf_layer_desc>();
+    void* q = a.ptr(); void* q_off = a.ptr(); int32_t q_stored = a.i32(); void* q_new = a.ptr();
+    const cf_q4_store* store = a.structure<cf_q4_store>(); void* k1 = a.ptr(); void* v1 = a.ptr();
+    void* segs = a.ptr(); void* n_seg = a.ptr(); int32_t seg_stride = a.i32(), batch = a.i32(), max_tq = a.i32(); int64_t max_kv = a.i64();
+    void* out = a.ptr(); void* mass = a.ptr(); void* score = a.ptr(); int32_t score_stride = a.i32();
+    void* ws = a.ptr(); int64_t ws_bytes = a.i64(); void* flag = a.ptr(); void* stream = a.stream();
+    return finish(a, [&] {
+        return cf_prefill_attention_q4(desc, q, (const int32_t*)q_off, q_stored, (const int32_t*)q_new, store, k1, v1, (const cf_segment*)segs,
+                                       (const int32_t*)n_seg, seg_stride, batch, max_tq, max_kv, out, (float*)mass, (float*)score,
+                                       score_stride, ws, (size_t)ws_bytes, (int32_t*)flag, stream);
+    });
+}
+
+CF_PY(quantize_cache) {
+    Args a(args, nargs, 10, "quantize_cache");
+    const cf_layer_desc* desc = a.structure<cf_layer_desc>();
+    void* k = a.ptr(); void* v = a.ptr(); int32_t n = a.i32(); void* live = a.ptr(); void* slots = a.ptr(); void* shift = a.ptr();
+    const cf_q4_store* store = a.structure<cf_q4_store>(); void* flag = a.ptr(); void* stream = a.stream();
+    return finish(a, [&] {
+        return cf_quantize_cache(desc, k, v, n, (const int32_t*)live, (const int64_t*)slots, (const int32_t*)shift, store, (int32_t*)flag, stream);
+    });
+}
+
+CF_PY(assemble_cache_q4) {
+    Args a(args, nargs, 21, "assemble_cache_q4");
+    const cf_layer_desc* desc = a.structure<cf_layer_desc>();
+    const cf_q4_store* store = a.structure<cf_q4_store>(); void* k1 = a.ptr(); void* v1 = a.ptr(); void* q_off = a.ptr();
+    void* segs = a.ptr(); void* n_seg = a.ptr(); int32_t seg_stride = a.i32(), batch = a.i32(), max_tq = a.i32(), max_len = a.i32();
+    void* off = a.ptr(); int64_t cap = a.i64(), ts = a.i64(), hs = a.i64(); void* kf = a.ptr(); void* vf = a.ptr();
+    void* len = a.ptr(); void* pos = a.ptr(); void* flag = a.ptr(); void* stream = a.stream();
+    return finish(a, [&] {
+        return cf_assemble_cache_q4(desc, store, k1, v1, (const int32_t*)q_off, (const cf_segment*)segs, (const int32_t*)n_seg, seg_stride,
+                                    batch, max_tq, max_len, (const int64_t*)off, cap, ts, hs, kf, vf, (int32_t*)len, (int32_t*)pos,
+                                    (int32_t*)flag, stream);
+    });
+}
+
+CF_PY(block_tables) {
+    Args a(args, nargs, 27, "block_tables");
+    void* cached = a.ptr(); void* fresh = a.ptr(); int32_t batch = a.i32(), block = a.i32(), n_blocks = a.i32(); int64_t first = a.i64();
+    void* table = a.ptr(); int32_t table_stride = a.i32(); void* free_blocks = a.ptr(); void* n_free = a.ptr(); void* position = a.ptr();
+    void* base = a.ptr(); void* n_base = a.ptr(); int32_t base_stride = a.i32(), q_stored = a.i32(); void* next_len = a.ptr();
+    void* next_free = a.ptr(); void* q_off = a.ptr(); void* q_new = a.ptr(); void* slots = a.ptr(); void* shift = a.ptr();
+    int64_t max_new = a.i64(); void* segs = a.ptr(); void* n_seg = a.ptr(); int32_t seg_stride = a.i32(); void* flag = a.ptr();
+    void* stream = a.stream();
+    return finish(a, [&] {
+        return cf_block_tables((const int32_t*)cached, (const int32_t*)fresh, batch, block, n_blocks, first, (int32_t*)table, table_stride,
+                               (int32_t*)free_blocks, (const int32_t*)n_free, (const int32_t*)position, (const cf_segment*)base,
+                               (const int32_t*)n_base, base_stride, q_stored, (int32_t*)next_len, (int32_t*)next_free, (int32_t*)q_off,
+                               (int32_t*)q_new, (int64_t*)slots, (int32_t*)shift, max_new, (cf_segment*)segs, (int32_t*)n_seg, seg_stride,
+                               (int32_t*)flag, stream);
+    });
+}
+
 CF_PY(prune_topk) {
     Args a(args, nargs, 11, "prune_topk");
     void* score = a.ptr(); void* len = a.ptr(); void* cand = a.ptr(); void* n_cand = a.ptr();
@@ -217,7 +273,8 @@ CF_PY(gather_segments) {
 #define CF_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {CF_METHOD(prefill_attention), CF_METHOD(prefill_attention_static), CF_METHOD(prefill_layer),
                            CF_METHOD(reposition_keys), CF_METHOD(assemble_cache), CF_METHOD(prune_topk),
-                           CF_METHOD(assign_positions), CF_METHOD(gather_segments), {nullptr, nullptr, 0, nullptr}};
+                           CF_METHOD(assign_positions), CF_METHOD(gather_segments), CF_METHOD(prefill_attention_q4),
+                           CF_METHOD(quantize_cache), CF_METHOD(assemble_cache_q4), CF_METHOD(block_tables), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_cfcall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

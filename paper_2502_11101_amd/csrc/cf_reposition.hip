@@ -69,6 +69,23 @@ template <> struct Chunk8<CF_F32> {
     }
 };
 
+// The eight values at element `idx` of a store in 4 bits (idx a multiple of 8): codes at idx / 2, their scale byte at idx / 32.
+template <int DT>
+__device__ __forceinline__ void load_q4(Chunk8<DT>& c, const void* codes, const uint8_t* scales, int64_t idx) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(codes) + (idx >> 1));
+    const float scale = __uint_as_float((uint32_t)scales[idx >> 5] << 23);
+    if constexpr (DT == CF_BF16)
+        c.r = U4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+    else
+        c.r = U4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3))};
+}
+
 // A work item is 8 pairs of one (token, kv head): under half-split pairing the 8 first elements [8j, 8j+8) and
 // their partners [d/2+8j, ...); under interleaved pairing 16 consecutive elements.  Items of a run of tokens are
 // numbered along the memory of the layout - token rows of one head after another where a head's tokens lie together
@@ -235,7 +252,8 @@ cf_status launch_dt(const cf_layer_desc* d, const RopeFreq& f, const void* k_in,
 // entries before its own; where it reads depends on its own entry alone, so its first loads are under way while
 // the entries are added up and the cos/sin pairs worked out.  Per (token, kv head, 8-pair item) two 16-byte K
 // chunks are rotated and two V chunks copied, from the store's (or the own block's) layout to the decode cache's.
-template <int DT, int PAIRING, int U>
+// Q4: the store is in 4 bits; a chunk is four bytes of codes and a scale byte, its values exact in the 16-bit type.
+template <int DT, int PAIRING, int U, bool Q4>
 __global__ __launch_bounds__(kThreads) void assemble_kernel(AssembleArgs a, RopeFreq freq) {
     __shared__ float2 cs[kMaxHalf];
     __shared__ int s_before, s_total, s_bad, s_off_range;
@@ -322,10 +340,19 @@ __global__ __launch_bounds__(kThreads) void assemble_kernel(AssembleArgs a, Rope
             j[u] = i.j;
             const int64_t src = (seg.tok_offset + tok[u]) * in_ts + (int64_t)i.head * in_hs;
             const int o0 = first_of<PAIRING>(i.j), o1 = second_of<PAIRING>(i.j, half);
-            x[u].load(k_in, src + o0);
-            y[u].load(k_in, src + o1);
-            va[u].load(v_in, src + o0);
-            vb[u].load(v_in, src + o1);
+            if (Q4 && !self) {
+                if constexpr (Q4) {
+                    load_q4(x[u], k_in, a.k_scales, src + o0);
+                    load_q4(y[u], k_in, a.k_scales, src + o1);
+                    load_q4(va[u], v_in, a.v_scales, src + o0);
+                    load_q4(vb[u], v_in, a.v_scales, src + o1);
+                }
+            } else {
+                x[u].load(k_in, src + o0);
+                y[u].load(k_in, src + o1);
+                va[u].load(v_in, src + o0);
+                vb[u].load(v_in, src + o1);
+            }
         }
         if (first) {
             if (!add_up()) return;                       // the whole block
@@ -347,7 +374,7 @@ __global__ __launch_bounds__(kThreads) void assemble_kernel(AssembleArgs a, Rope
     }
 }
 
-template <int DT, int PAIRING, int U>
+template <int DT, int PAIRING, int U, bool Q4>
 cf_status launch_assemble_piece(const cf_layer_desc* d, const RopeFreq& f, const AssembleArgs& a, int32_t max_seg_len,
                                 hipStream_t s) {
     const int64_t entries = (int64_t)a.batch * a.seg_stride;
@@ -355,20 +382,20 @@ cf_status launch_assemble_piece(const cf_layer_desc* d, const RopeFreq& f, const
     // tokens: 85.5 -> 62.9 and 278 -> 127 us; up to 300 entries no difference)
     const int64_t most = a.seg_stride > kThreads ? kMostBlocks * kThreads / a.seg_stride : kMostBlocks;
     const dim3 grid((unsigned)entries, pieces(entries, max_seg_len, d->n_kv_heads * (d->head_dim / 16), U, most));
-    hipLaunchKernelGGL((assemble_kernel<DT, PAIRING, U>), grid, dim3(kThreads), 0, s, a, f);
+    hipLaunchKernelGGL((assemble_kernel<DT, PAIRING, U, Q4>), grid, dim3(kThreads), 0, s, a, f);
     CF_HIP(hipGetLastError());
     return CF_OK;
 }
 
-template <int DT, int PAIRING>
+template <int DT, int PAIRING, bool Q4 = false>
 cf_status launch_assemble_dt(const cf_layer_desc* d, const RopeFreq& f, const AssembleArgs& a, int32_t max_seg_len,
                              hipStream_t s) {
     // Two items per thread share a block's table sums and cos/sin pairs, but leave half as many blocks.  From 1024 blocks of
     // one on they are faster (30 documents x 160 tokens of 32 heads, bf16: 33.7 against 35.8 us; 5 queries x 7
     // documents of 199 and more tokens, 4 heads: 10.6 against 10.9), below it slower (under 7 us: by 0.1-0.5 us).
     const int64_t items = (int64_t)a.batch * a.seg_stride * max_seg_len * d->n_kv_heads * (d->head_dim / 16);
-    if (items < (int64_t)256 * 4 * kThreads) return launch_assemble_piece<DT, PAIRING, 1>(d, f, a, max_seg_len, s);
-    return launch_assemble_piece<DT, PAIRING, 2>(d, f, a, max_seg_len, s);
+    if (items < (int64_t)256 * 4 * kThreads) return launch_assemble_piece<DT, PAIRING, 1, Q4>(d, f, a, max_seg_len, s);
+    return launch_assemble_piece<DT, PAIRING, 2, Q4>(d, f, a, max_seg_len, s);
 }
 
 template <class F> cf_status by_pairing(const cf_layer_desc* d, F&& go) {
@@ -380,6 +407,10 @@ template <class F> cf_status by_pairing(const cf_layer_desc* d, F&& go) {
 
 cf_status launch_assemble(const cf_layer_desc* d, const RopeFreq& f, const AssembleArgs& a, int32_t max_seg_len,
                           hipStream_t s) {
+    if (a.k_scales) {
+        if (d->dtype == CF_BF16) return by_pairing(d, [&](auto P) { return launch_assemble_dt<CF_BF16, P.value, true>(d, f, a, max_seg_len, s); });
+        return by_pairing(d, [&](auto P) { return launch_assemble_dt<CF_F16, P.value, true>(d, f, a, max_seg_len, s); });
+    }
     switch (d->dtype) {
         case CF_F32: return by_pairing(d, [&](auto P) { return launch_assemble_dt<CF_F32, P.value>(d, f, a, max_seg_len, s); });
         case CF_BF16: return by_pairing(d, [&](auto P) { return launch_assemble_dt<CF_BF16, P.value>(d, f, a, max_seg_len, s); });

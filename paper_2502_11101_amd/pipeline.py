@@ -46,6 +46,86 @@ def store_to_device(x: np.ndarray, dtype: str, layout: str, pad_tokens: int = 0,
     return t
 
 
+class Q4Store:
+    """A cache store in 4 bits for one layer: 68 bytes per (token, kv head) row of keys and of values instead of 256.
+
+    Owns the code and scale arrays ([token][kv head][.] or, head-major, [kv head][token][.]); ``desc`` is the layer's descriptor with
+    this store's strides, ``store`` what the calls take.
+    """
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, dtype: str, rope_base: float, max_positions: int, n_tokens: int,
+                 layout: str = "head", rope_pairing: int = cf.CF_ROPE_HALF, softmax_scale: float = 0.0, device="cuda"):
+        ts, hs = store_strides(n_tokens, n_kv_heads, 128, layout)
+        self.desc = cf.make_desc(n_q_heads, n_kv_heads, 128, dtype, rope_base, max_positions, rope_pairing, softmax_scale,
+                                 store_token_stride=ts, store_head_stride=hs)
+        self.n_tokens = int(n_tokens)
+        lead = (n_tokens, n_kv_heads) if layout == "token" else (n_kv_heads, n_tokens)
+        new = lambda n: torch.zeros((*lead, n), dtype=torch.uint8, device=device)
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = new(64), new(4), new(64), new(4)
+        self.store = cf.make_q4_store(self.k_codes, self.k_scales, self.v_codes, self.v_scales, self.n_tokens)
+
+    def write(self, k, v, slots, shift=None, dev_flag=None, n_live=None) -> None:
+        """Rows of fresh keys and values to their slots, keys turned by `shift` positions (int32 per row) ahead of it; rows at and past
+        `n_live` (device int32) are padding."""
+        cf.cf_quantize_cache(self.desc, k, v, int(k.shape[0]), slots, shift, self.store, dev_flag, None, n_live)
+
+
+class BlockCache:
+    """Decode caches of `batch` requests in blocks of a 4-bit store that they share: the tables of a step, for every layer.
+
+    A step: ``step(fresh)`` with every request's new tokens (device int32 [batch]; 0 none, negative: the request leaves), then per
+    layer ``attend`` and ``append`` with that layer's store.  Blocks are handed out of store tokens
+    [first_token, first_token + n_blocks * block_tokens).  ``base_segs`` / ``n_base``: entries that lead a request's table (the shared
+    prefix and documents); ``position``: position of its first own token.  Row t of a request's q / k / v carries RoPE for local position t.
+    """
+
+    def __init__(self, desc: cf.cf_layer_desc, batch: int, block_tokens: int, n_blocks: int, max_len: int, max_new: int,
+                 first_token: int = 0, base_segs=None, n_base=None, base_stride: int = 0, max_base_tokens: int = 0, position=None,
+                 device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.desc, self.batch, self.block_tokens, self.n_blocks, self.first_token = desc, batch, block_tokens, n_blocks, first_token
+        self.base_segs, self.n_base, self.base_stride, self.position = base_segs, n_base, base_stride, position
+        self.max_new = max_new                  # rows of one request in one step
+        self.table_stride = -(-max_len // block_tokens)
+        self.seg_stride = base_stride + self.table_stride + 1
+        self.max_rows = batch * max_new
+        self.table = torch.zeros((batch, self.table_stride), **i32)
+        self.free_blocks = torch.arange(n_blocks - 1, -1, -1, **i32)
+        self.n_free, self.next_n_free = torch.full((1,), n_blocks, **i32), torch.zeros((1,), **i32)
+        self.len, self.next_len = torch.zeros((batch,), **i32), torch.zeros((batch,), **i32)
+        self.q_off, self.q_new = torch.zeros((batch + 1,), **i32), torch.zeros((batch,), **i32)
+        self.slots = torch.full((self.max_rows,), -1, dtype=torch.int64, device=device)
+        self.shift = torch.zeros((self.max_rows,), **i32)
+        self.segs = torch.zeros((batch, self.seg_stride, 32), dtype=torch.uint8, device=device)
+        self.n_seg = torch.zeros((batch,), **i32)
+        self.dev_flag = torch.zeros((1,), **i32)
+        self.max_kv_tokens = max_base_tokens + max_len
+        self.ws_bytes = cf.cf_prefill_workspace_bytes_q4(desc, batch, max_new, self.seg_stride, self.max_kv_tokens)
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
+
+    def step(self, fresh) -> None:
+        """The tables of a step in which the requests add `fresh` tokens; the rows of all requests lie back to back, in order."""
+        cf.cf_block_tables(self.len, fresh, self.batch, self.block_tokens, self.n_blocks, self.first_token, self.table, self.table_stride,
+                           self.free_blocks, self.n_free, self.position, self.base_segs, self.n_base, self.base_stride, 0, self.next_len,
+                           self.next_n_free, self.q_off, self.q_new, self.slots, self.shift, self.max_rows, self.segs, self.n_seg,
+                           self.seg_stride, self.dev_flag)
+        self.len, self.next_len = self.next_len, self.len
+        self.n_free, self.next_n_free = self.next_n_free, self.n_free
+
+    def attend(self, layer: Q4Store, q, k, v, out) -> None:
+        """out = attention of the step's rows over the requests' shared entries, cached tokens and, causally, themselves."""
+        cf.cf_prefill_attention_q4(layer.desc, q, self.q_off, 0, self.q_new, layer.store, k, v, self.segs, self.n_seg, self.seg_stride,
+                                   self.batch, self.max_new, self.max_kv_tokens, out, None, None, 1, self.workspace, self.ws_bytes,
+                                   self.dev_flag)
+
+    def append(self, layer: Q4Store, k, v) -> None:
+        """The step's keys, turned to their positions, and values go to their slots (k, v: the step's rows, and any padding behind them)."""
+        layer.write(k, v, self.slots, self.shift, self.dev_flag, self.q_off[self.batch:])
+
+    def flags(self) -> int:
+        return int(self.dev_flag.item())
+
+
 class PrefillBatch:
     """Device tables of ``batch`` queries, each with up to ``stride`` candidate documents.
 
@@ -94,6 +174,7 @@ class PrefillBatch:
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)   # contents are scratch
         self.n_alive = self.stride
         self.n_pending = 0          # layers whose scores are still pending in the workspace (layer(defer=True))
+        self._q4 = None             # workspace of attention_q4 and its size
         self._cache = None          # device addresses and the prune-step structs of the current tables (layer())
 
     # -- Alg. 2 init: every document is a candidate, placement order = retriever order
@@ -113,6 +194,15 @@ class PrefillBatch:
                                 self.batch, self.tq, self.max_kv_tokens, out, self.mass,
                                 self.score if accumulate else None, self.stride, self.workspace, self.ws_bytes,
                                 self.dev_flag)
+
+    # -- the same over a store in 4 bits (whose descriptor replaces the batch's)
+    def attention_q4(self, q, k_self, v_self, layer: Q4Store, out, accumulate: bool = True) -> None:
+        if self._q4 is None:
+            n = cf.cf_prefill_workspace_bytes_q4(layer.desc, self.batch, self.tq, self.seg_stride, self.max_kv_tokens)
+            self._q4 = (torch.zeros(n, dtype=torch.uint8, device=self.device), n)
+        cf.cf_prefill_attention_q4(layer.desc, q, self.q_off, self.q_stored_start, self.q_start, layer.store, k_self, v_self, self.segs,
+                                   self.n_seg, self.seg_stride, self.batch, self.tq, self.max_kv_tokens, out, self.mass,
+                                   self.score if accumulate else None, self.stride, *self._q4, self.dev_flag)
 
     # -- Alg. 2: ids_sort = argsort(S); ids = prun(ids_sort); then Sec. 2.5 re-allocation.
     # Writes the next layer's tables; the current ones stay valid until advance().
@@ -220,6 +310,10 @@ class StoreBuilder:
         self.write_segs = cf.segments_to_device(cf.segments_array(own), device)
         self.write_n = torch.ones((self.n,), **i32)
         self.final_off = torch.from_numpy(np.asarray(store_off, dtype=np.int64)).to(device)
+        # the store token and the move of every row (write_q4)
+        row = np.arange(self.total) - np.repeat(q_off[:-1], lens)
+        self.slots = torch.from_numpy(np.repeat(np.asarray(store_off, dtype=np.int64), lens) + row).to(device)
+        self.shift = torch.from_numpy(np.repeat(np.asarray(positions, dtype=np.int32), lens)).to(device)
         self.final_len = torch.zeros((self.n,), **i32)
         self.dev_flag = torch.zeros((1,), **i32)
         self.max_kv_tokens = self.prefix_len + self.max_len
@@ -238,6 +332,10 @@ class StoreBuilder:
         cf.cf_assemble_cache(self.desc, None, None, 0, k, v, self.q_off, self.write_segs, self.write_n, 1, self.n,
                              self.max_len, self.max_len, self.final_off, self.n_store_tokens, store_token_stride,
                              store_head_stride, k_store, v_store, self.final_len, None, self.dev_flag)
+
+    def write_q4(self, k, v, layer: Q4Store) -> None:
+        """The same into a store in 4 bits: keys, turned to their cached positions, and values go to the texts' places."""
+        layer.write(k, v, self.slots, self.shift, self.dev_flag)
 
     def flags(self) -> int:
         return int(self.dev_flag.item())

@@ -1,0 +1,336 @@
+"""Attention over a 4-bit cache store (cf_prefill_attention_q4) against the oracle on the values that the store stands for."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cachefocus_oracle as orc
+from paper_2502_11101_amd import binding as cf
+from paper_2502_11101_amd import pipeline as pl
+from paper_2502_11101_amd import workloads as wl
+from tests import helpers as H
+from tests import q4_reference as R
+
+pytestmark = pytest.mark.gpu
+
+BASE, POSITIONS = 1.0e4, 1 << 20
+PAIRING = {"half": cf.CF_ROPE_HALF, "interleaved": cf.CF_ROPE_INTERLEAVED}
+i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def upload(host, heads, dtype, layout, pairing, scale=0.0, group=1, pad=0):
+    """Q4Store of host arrays [token][head][.]; `pad`: unused tokens behind every head's."""
+    n = host["k_codes"].shape[0]
+    s = pl.Q4Store(heads * group, heads, dtype, BASE, POSITIONS, n + pad, layout, PAIRING[pairing], scale)
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        x = torch.from_numpy(np.ascontiguousarray(host[name] if layout == "token" else host[name].transpose(1, 0, 2)))
+        getattr(s, name)[:n].copy_(x) if layout == "token" else getattr(s, name)[:, :n].copy_(x)
+    return s
+
+
+def check(hq, hkv, tables, lengths, dtype="bf16", pairing="half", layout="head", seed=0, n_store=600, scale=None, change=None, own_first=False,
+          max_kv=None, spare_entries=0, no_own=(), compare=None, q_pos=None):
+    """`tables`: per query (offset, length, stored, new) of its store entries; `lengths`: its rows, whose own block follows."""
+    rng = np.random.default_rng(seed)
+    batch, tq = len(tables), max(max(lengths), 1)
+    host = R.random_store(rng, n_store, hkv, dtype)
+    total = sum(lengths)
+    normal = lambda n, h: wl.round_to_dtype(rng.standard_normal((n, h, 128), dtype=np.float32), dtype)
+    t = dict(q=normal(total, hq), k_self=normal(total, hkv), v_self=normal(total, hkv))
+    if change is not None:
+        change(host, t, rng)
+    s = upload(host, hkv, dtype, layout, pairing, 0.0 if scale is None else scale, hq // hkv, pad=3)
+    q_off = np.concatenate([[0], np.cumsum(lengths)]).astype(int)
+    q_pos = [5000 + 7 * b for b in range(batch)] if q_pos is None else q_pos
+    segs, rows = [], []
+    stride = max(len(x) for x in tables) + 1 + spare_entries
+    for b, x in enumerate(tables):
+        own = [orc.Segment(o, n, a, p, orc.KIND_DOC, i % 3) for i, (o, n, a, p) in enumerate(x)]
+        me = [] if b in no_own else [orc.Segment(int(q_off[b]), lengths[b], 0, q_pos[b], orc.KIND_SELF, -1)]
+        own = me + own if own_first else own + me
+        segs.append(own)
+        rows += [(g.tok_offset, g.len, g.stored_start, g.new_start, g.kind, g.doc) for g in own] + [(7, 1 << 30, -1, -1, 9, 5)] * (stride - len(own))
+    kv = max(sum(g.len for g in x) for x in segs) if max_kv is None else max_kv
+    need = cf.cf_prefill_workspace_bytes_q4(s.desc, batch, tq, stride, kv)
+    dev = {k: pl.to_device(v, dtype) for k, v in t.items()}
+    table, n_seg = cf.segments_to_device(cf.segments_array(rows)), i32([len(x) for x in segs])
+    results = []
+    for masses in (False, True):
+        ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+        out = torch.full((total + 2, hq, 128), 55.0, dtype=pl.TORCH_DTYPE[dtype], device="cuda")
+        flag, mass, score = i32([0]), torch.full((batch, stride), 99.0, device="cuda"), torch.ones((batch, 4), device="cuda")
+        cf.cf_prefill_attention_q4(s.desc, dev["q"], i32(q_off.tolist()), 0, i32(q_pos), s.store, dev["k_self"], dev["v_self"], table, n_seg,
+                                   stride, batch, tq, kv, out, mass if masses else None, score if masses else None, 4, ws, need, flag)
+        torch.cuda.synchronize()
+        assert int(flag.item()) == 0 and bool((ws[need:] == 0xFF).all()) and bool((out[total:] == 55).all())
+        results.append(out[:total])
+    a, b = results
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16))       # the same with masses and without
+    got, mass, score = results[1].double().cpu().numpy(), mass.cpu().numpy().astype(np.float64), score.cpu().numpy()
+    ks, vs = R.decode(host["k_codes"], host["k_scales"]), R.decode(host["v_codes"], host["v_scales"])
+    for b in range(batch) if compare is None else compare:
+        part = slice(q_off[b], q_off[b + 1])
+        n = len(segs[b])
+        assert (mass[b, n:] == 99).all()
+        if lengths[b] == 0:
+            assert (mass[b, :n] == 0).all()
+            continue
+        own = t["k_self"], t["v_self"]
+        store_segs = [g for g in segs[b] if g.kind != orc.KIND_SELF]
+        ck, cv, compact = H.compact_query(segs[b], ks, vs) if store_segs else (None, None, segs[b])
+        if not sum(g.len for g in segs[b]):
+            assert (got[part] == 0).all() and (mass[b, :n] == 0).all()
+            continue
+        out, ref_mass, out_off, mass_off = R.attention(t["q"][part], q_pos[b], ck, cv, *own, compact, hkv, BASE, pairing, scale)
+        assert (np.abs(got[part] - out) <= R.HALF_STEP[dtype] * np.abs(out) + out_off + 1e-6 * np.abs(out).max()).all(), b
+        assert (np.abs(mass[b, :n] - ref_mass) <= mass_off + 1e-30).all(), b
+        assert abs(mass[b, :n].sum() - hq * lengths[b]) <= 1e-5 * hq * lengths[b]
+        want = np.ones(4)
+        for g, m in zip(segs[b], mass[b]):
+            if g.doc >= 0:
+                want[g.doc] += m
+        assert np.allclose(score[b], want, rtol=1e-5)
+    return got, mass
+
+
+def docs(rng, n, lo, hi, n_store=600, moved=True):
+    out, at = [], 100
+    for _ in range(n):
+        m = int(rng.integers(lo, hi + 1))
+        out.append((int(rng.integers(0, n_store - m + 1)), m, 40, at if moved else 40))
+        at += m
+    return out
+
+
+RNG = np.random.default_rng(99)
+CASES = {
+    # one row over one entry, of one token and of many
+    "one_token": dict(hq=2, hkv=2, tables=[[(5, 1, 0, 0)]], lengths=[1]),
+    "decode": dict(hq=4, hkv=4, tables=[[(3, 500, 0, 0)], [(0, 31, 0, 0)], [(100, 33, 0, 0)]], lengths=[1, 1, 1]),
+    "decode_group": dict(hq=14, hkv=2, tables=[[(3, 597, 0, 0)], [(0, 64, 0, 0)]], lengths=[1, 1], dtype="f16"),
+    "decode_wide_group": dict(hq=40, hkv=2, tables=[[(3, 300, 0, 9)]], lengths=[1]),
+    # rows at the edges of a block, of two, of a wavefront's share, of a workgroup's
+    **{f"rows_{n}": dict(hq=1, hkv=1, tables=[docs(RNG, 4, 1, 90)], lengths=[n]) for n in (15, 16, 17, 32, 33, 64, 65, 128, 129, 256, 257, 300)},
+    # an own block alone, at and past a tile
+    **{f"own_{n}": dict(hq=2, hkv=1, tables=[[]], lengths=[n], dtype="f16") for n in (1, 31, 32, 33, 100)},
+    "own_first": dict(hq=4, hkv=2, tables=[docs(RNG, 3, 10, 60), docs(RNG, 2, 1, 9)], lengths=[40, 3], own_first=True),
+    "no_own_block": dict(hq=4, hkv=2, tables=[docs(RNG, 3, 10, 60)], lengths=[9], no_own=(0,)),
+    # lengths of zero: entries, queries, both
+    "empty_entries": dict(hq=4, hkv=2, tables=[[(0, 0, 0, 0), (9, 40, 0, 3), (50, 0, 1, 2), (600, 0, 0, 0), (3, 1, 4, 4)], []], lengths=[5, 2]),
+    "empty_query": dict(hq=4, hkv=4, tables=[docs(RNG, 2, 9, 40), docs(RNG, 2, 9, 40), docs(RNG, 1, 9, 40)], lengths=[0, 7, 0]),
+    "nothing_to_see": dict(hq=4, hkv=4, tables=[[(0, 0, 0, 0)], docs(RNG, 2, 9, 40)], lengths=[3, 2], no_own=(0,)),
+    "ragged_batch": dict(hq=6, hkv=2, tables=[docs(RNG, n, 1, 80) for n in (1, 5, 9, 2)], lengths=[11, 1, 29, 17]),
+    "token_major": dict(hq=6, hkv=3, tables=[docs(RNG, 5, 20, 60)], lengths=[21], layout="token", dtype="f16"),
+    "interleaved": dict(hq=6, hkv=3, tables=[docs(RNG, 5, 20, 60)], lengths=[21], pairing="interleaved"),
+    "interleaved_token_major": dict(hq=8, hkv=1, tables=[docs(RNG, 5, 20, 60)] * 2, lengths=[1, 2], pairing="interleaved", layout="token", dtype="f16"),
+    # tables past the registers' 64 entries, of single tokens, and the longest
+    "many_entries": dict(hq=2, hkv=2, tables=[docs(RNG, 100, 1, 12)], lengths=[20]),
+    "single_tokens": dict(hq=4, hkv=2, tables=[docs(RNG, 63, 1, 1)], lengths=[1]),
+    "most_entries": dict(hq=2, hkv=1, tables=[docs(RNG, 255, 1, 7)], lengths=[1], dtype="f16"),
+    # far positions, both ways
+    "far": dict(hq=2, hkv=2, tables=[[(0, 90, 0, POSITIONS - 90), (90, 64, POSITIONS - 200, 5), (200, 1, 3, 3)]], lengths=[9], q_pos=[POSITIONS // 2]),
+    "long": dict(hq=2, hkv=1, tables=[[(0, 6000, 0, 0)], [(100, 5900, 0, 0)]], lengths=[1, 1], n_store=6000),
+    "long_rows": dict(hq=8, hkv=1, tables=[[(0, 3000, 0, 9), (3000, 2999, 0, 3)]], lengths=[9], n_store=6000),
+    "bound_above_the_list": dict(hq=4, hkv=4, tables=[docs(RNG, 2, 9, 40)], lengths=[3], max_kv=100000, spare_entries=30),
+}
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_against_the_oracle(name):
+    check(**CASES[name], seed=len(name))
+
+
+@pytest.mark.parametrize("scale", [0.02, 0.7])
+@pytest.mark.parametrize("pairing", ["half", "interleaved"])
+def test_softmax_scales(scale, pairing):
+    check(4, 2, [docs(np.random.default_rng(3), 6, 20, 90)], [13], scale=scale, pairing=pairing)
+
+
+def test_scores_that_rise_tile_after_tile():
+    """The row maximum moves in every tile, by far more than the range of a stale reference."""
+    def change(host, t, rng):
+        n, heads = host["k_codes"].shape[:2]
+        k = np.tile(t["q"][:1, ::2].astype(np.float64), (n, 1, 1)) * np.linspace(0.0, 3.0, n)[:, None, None]
+        host["k_codes"], host["k_scales"], _ = R.encode(k, "bf16")
+    check(4, 2, [[(0, 600, 0, 0)], [(0, 600, 0, 0)]], [3, 1], change=change, q_pos=[0, 0])
+
+
+@pytest.mark.parametrize("dtype,low,high", [("bf16", -100, 100), ("bf16", -30, -20), ("f16", -23, 13), ("bf16", -24, 14)])
+def test_scales_of_any_size(dtype, low, high):
+    """Rows whose scales are at the ends of the type's range and far outside fp16's, among ordinary ones: in values everywhere, in keys
+    where the scores stay finite."""
+    def change(host, t, rng):
+        n = host["v_codes"].shape[0]
+        odd = rng.random(n) < 0.2
+        odd[:64] = False
+        e = rng.integers(low, high + 1, size=host["v_scales"].shape)
+        host["v_scales"] = np.where(odd[:, None, None], e + 127, host["v_scales"]).astype(np.uint8)
+        small = rng.random(n) < 0.1
+        host["k_scales"] = np.where(small[:, None, None], np.minimum(e, 0) + 127, host["k_scales"]).astype(np.uint8)
+    for tables, lengths in (([docs(np.random.default_rng(1), 6, 20, 90)], [20]), ([[(0, 600, 0, 0)]], [1])):
+        check(4, 2, tables, lengths, dtype=dtype, change=change, seed=low + 200)
+
+
+def test_queries_of_any_size():
+    def change(host, t, rng):
+        t["q"] = wl.round_to_dtype((t["q"] * np.exp2(rng.integers(-40, 3, size=t["q"].shape[:2]))[..., None]).astype(np.float32), "bf16")
+        t["q"][3] = 0
+    check(4, 2, [docs(np.random.default_rng(2), 6, 20, 90)], [20], change=change)
+
+
+def _call(s, dev, q_off, q_pos, rows, counts, stride, batch, tq, kv, out, mass=None, flag=None, stream=None, ws=None, n_store=None):
+    need = cf.cf_prefill_workspace_bytes_q4(s.desc, batch, tq, stride, kv)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda") if ws is None else ws
+    cf.cf_prefill_attention_q4(s.desc, dev["q"], i32(q_off), 0, i32(q_pos), s.store, dev["k_self"], dev["v_self"],
+                               cf.segments_to_device(cf.segments_array(rows)), i32(counts), stride, batch, tq, kv, out, mass, None, 1, ws, need,
+                               flag, stream)
+    return ws
+
+
+def _small(hq=4, hkv=2, tq=6, n_store=200, dtype="bf16", seed=0):
+    rng = np.random.default_rng(seed)
+    host = R.random_store(rng, n_store, hkv, dtype)
+    normal = lambda n, h: wl.round_to_dtype(rng.standard_normal((n, h, 128), dtype=np.float32), dtype)
+    t = dict(q=normal(tq, hq), k_self=normal(tq, hkv), v_self=normal(tq, hkv))
+    return host, t, upload(host, hkv, dtype, "head", "half", group=hq // hkv), {k: pl.to_device(v, dtype) for k, v in t.items()}
+
+
+def test_nan_stays_where_it_is_read():
+    """A value group that is not a number reaches the channels it holds, a key row every channel, a query row its own output; rows past a
+    list's end and tokens that are not listed reach nothing, nor do later tokens of the own block."""
+    host, t, s, _ = _small(tq=40, hq=2, hkv=2)
+    s.v_scales[:, 150:] = 255                            # not listed
+    s.k_scales[:, 101:] = 255
+    t["v_self"][20, 0, 9] = np.inf                       # seen by rows 20 .. only
+    t["v_self"][35:] = np.nan
+    t["k_self"][37] = -np.inf
+    dev = {k: pl.to_device(v, "bf16") for k, v in t.items()}
+    rows = [(0, 101, 0, 0, cf.CF_SEG_DOC, 0), (0, 40, 0, 300, cf.CF_SEG_SELF, -1)]
+    out, flag = torch.empty_like(dev["q"]), i32([0])
+    _call(s, dev, [0, 40], [300], rows, [2], 2, 1, 40, 141, out, flag=flag)
+    torch.cuda.synchronize()
+    assert int(flag.item()) == 0
+    got = out.float().cpu().numpy()
+    assert np.isfinite(got[:20]).all() and np.isnan(got[35:]).all()
+    assert (got[20:35, 0, 9] == np.inf).all() and np.isfinite(np.delete(got[20:35, 0], 9, axis=-1)).all() and np.isfinite(got[20:35, 1]).all()
+    # a group of a listed token's values
+    s.v_scales[1, 60, 2] = 255
+    rows = rows[:1]
+    _call(s, dev, [0, 40], [300], rows, [1], 1, 1, 40, 141, out)
+    torch.cuda.synchronize()
+    got = out.float().cpu().numpy()
+    assert np.isfinite(got[:, 0]).all() and np.isnan(got[:, 1, 64:96]).all() and np.isfinite(got[:, 1, :64]).all() and np.isfinite(got[:, 1, 96:]).all()
+    # a listed key; a query row
+    s.v_scales[1, 60, 2] = 127
+    s.k_scales[0, 7, 1] = 255
+    t["q"][5, 1, 3] = np.nan
+    dev["q"] = pl.to_device(t["q"], "bf16")
+    _call(s, dev, [0, 40], [300], rows, [1], 1, 1, 40, 141, out)
+    torch.cuda.synchronize()
+    got = out.float().cpu().numpy()
+    assert np.isnan(got[:, 0]).all() and np.isnan(got[5, 1]).all() and np.isfinite(np.delete(got[:, 1], 5, axis=0)).all()
+
+
+@pytest.mark.parametrize("entry,flag", [
+    ((0, -1, 0, 0, 1, 0), cf.CF_FLAG_BAD_SEGMENT), ((-1, 5, 0, 0, 1, 0), cf.CF_FLAG_BAD_SEGMENT), ((190, 11, 0, 0, 1, 0), cf.CF_FLAG_BAD_SEGMENT),
+    ((0, 5, 0, 0, 7, 0), cf.CF_FLAG_BAD_SEGMENT), ((1 << 50, 5, 0, 0, 1, 0), cf.CF_FLAG_BAD_SEGMENT), ((3, 6, 0, 0, 2, -1), cf.CF_FLAG_BAD_SEGMENT),
+    ((0, 5, 0, POSITIONS - 4, 1, 0), cf.CF_FLAG_POS_RANGE), ((0, 5, -1, 0, 1, 0), cf.CF_FLAG_POS_RANGE)])
+def test_bad_entries_are_skipped_and_flagged(entry, flag):
+    host, t, s, dev = _small()
+    good = (20, 50, 0, 9, cf.CF_SEG_DOC, 1)
+    outs = []
+    for rows in ([good], [entry, good]):
+        out, f = torch.empty_like(dev["q"]), i32([0])
+        _call(s, dev, [0, 6], [100], rows + [(0, 0, 0, 0, 1, -1)] * (3 - len(rows)), [len(rows)], 3, 1, 6, 60, out, flag=f)
+        torch.cuda.synchronize()
+        outs.append((out.float().cpu().numpy(), int(f.item())))
+    assert outs[0][1] == 0 and outs[1][1] == flag
+    assert np.abs(outs[0][0] - outs[1][0]).max() <= 2 ** -6 * np.abs(outs[0][0]).max()
+
+
+def test_bad_counts_and_positions():
+    host, t, s, dev = _small()
+    good = (20, 50, 0, 9, cf.CF_SEG_DOC, 1)
+    for count, pos, want, empty in ((-3, 100, cf.CF_FLAG_BAD_SEGMENT, True), (9, 100, cf.CF_FLAG_BAD_SEGMENT, False), (1, POSITIONS, cf.CF_FLAG_POS_RANGE, True)):
+        out, f = torch.full_like(dev["q"], 3.0), i32([0])
+        _call(s, dev, [0, 6], [pos], [good] * 2, [count], 2, 1, 6, 100, out, flag=f)
+        torch.cuda.synchronize()
+        assert int(f.item()) == want and bool((out == 0).all()) == empty
+
+
+def test_offsets_past_32_bits():
+    """A store whose tokens lie further than 2^32 bytes apart (three heads, 2 GB of unused rows between them)."""
+    rng = np.random.default_rng(4)
+    heads, far = 3, 36_000_000                           # tokens of a head: 2.3 GB of codes, 144 MB of scales
+    host = R.random_store(rng, 70, heads, "bf16")
+    codes = {x: torch.zeros((heads * far, 64), dtype=torch.uint8, device="cuda") for x in "kv"}
+    scales = {x: torch.zeros((heads * far, 4), dtype=torch.uint8, device="cuda") for x in "kv"}
+    at = far - 75
+    for x in "kv":
+        for h in range(heads):
+            codes[x][h * far + at:h * far + at + 70] = torch.from_numpy(host[x + "_codes"][:, h].copy()).cuda()
+            scales[x][h * far + at:h * far + at + 70] = torch.from_numpy(host[x + "_scales"][:, h].copy()).cuda()
+    desc = cf.make_desc(heads, heads, 128, "bf16", BASE, POSITIONS, store_token_stride=128, store_head_stride=far * 128)
+    store = cf.make_q4_store(codes["k"], scales["k"], codes["v"], scales["v"], far)
+    q = wl.round_to_dtype(rng.standard_normal((2, heads, 128), dtype=np.float32), "bf16")
+    dq = pl.to_device(q, "bf16")
+    out, ws_bytes = torch.empty_like(dq), cf.cf_prefill_workspace_bytes_q4(desc, 1, 2, 1, 70)
+    ws, flag = torch.zeros(ws_bytes, dtype=torch.uint8, device="cuda"), i32([0])
+    cf.cf_prefill_attention_q4(desc, dq, i32([0, 2]), 0, i32([90]), store, None, None, cf.segments_to_device(cf.segments_array([(at, 70, 0, 0, 1, -1)])),
+                               i32([1]), 1, 1, 2, 70, out, None, None, 1, ws, ws_bytes, flag)
+    k, v = R.decode(host["k_codes"], host["k_scales"]), R.decode(host["v_codes"], host["v_scales"])
+    ref, _, off, _ = R.attention(q, 90, k, v, None, None, [orc.Segment(0, 70, 0, 0, orc.KIND_DOC, -1)], heads, BASE)
+    assert int(flag.item()) == 0
+    assert (np.abs(out.double().cpu().numpy() - ref) <= 2.0 ** -8 * np.abs(ref) + off + 1e-6).all()
+    # and written there, and gathered from there
+    cf.cf_quantize_cache(desc, pl.to_device(np.repeat(k[:1], 1, 0), "bf16"), pl.to_device(v[:1], "bf16"), 1, torch.tensor([far - 1], device="cuda"), None,
+                         store, flag)
+    kf, vf, n = torch.zeros((1, heads, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, heads, 128), dtype=torch.bfloat16, device="cuda"), i32([0])
+    cf.cf_assemble_cache_q4(desc, store, None, None, i32([0, 0]), cf.segments_to_device(cf.segments_array([(far - 1, 1, 0, 0, 1, -1)])), i32([1]), 1, 1, 1,
+                            1, torch.zeros(1, dtype=torch.int64, device="cuda"), 1, heads * 128, 128, kf, vf, n, None, flag)
+    assert int(flag.item()) == 0 and np.array_equal(kf.double().cpu().numpy(), k[:1]) and np.array_equal(vf.double().cpu().numpy(), v[:1])
+
+
+def test_runs_are_bit_identical_on_any_stream():
+    host, t, s, dev = _small(hq=8, hkv=2, tq=30, n_store=600)
+    rows = [(o, n, a, p, cf.CF_SEG_DOC, i) for i, (o, n, a, p) in enumerate(docs(np.random.default_rng(8), 9, 20, 60))] + [(0, 30, 0, 900, cf.CF_SEG_SELF, -1)]
+    outs = []
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    mass = [torch.zeros((1, len(rows)), device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    keep = []
+    for i in range(4):
+        out = torch.empty_like(dev["q"])
+        st = streams[i & 1]
+        with torch.cuda.stream(st):
+            keep.append(_call(s, dev, [0, 30], [900], rows, [len(rows)], len(rows), 1, 30, 700, out, mass[i], stream=st))
+        outs.append(out)
+    torch.cuda.synchronize()
+    for o, m in zip(outs, mass):
+        assert torch.equal(o.view(torch.int16), outs[0].view(torch.int16)) and torch.equal(m, mass[0])
+
+
+def test_prefill_batch_prunes_by_the_masses_of_a_4_bit_store():
+    """PrefillBatch over a 4-bit store: initial allocation, attention with masses, prune event, the next layer's table."""
+    cfg = wl.scaled(wl.CONFIGS["qwen2_7b_layer"], name="q4", n_store_docs=8, docs_per_query=8, n_planted=2, keep=3, tq=16)
+    g, st = cfg.geometry, wl.build_structure(cfg, seed=21)
+    t = wl.build_layer(cfg, st, seed=22)
+    layer = pl.Q4Store(g.n_q_heads, g.n_kv_heads, g.dtype, g.rope_base, g.max_positions, st.n_store_tokens)
+    every = torch.arange(st.n_store_tokens, device="cuda")
+    layer.write(pl.to_device(t["k_store"], g.dtype), pl.to_device(t["v_store"], g.dtype), every)
+    pb = pl.PrefillBatch(layer.desc, st.doc_off[:-1][st.query_docs], st.doc_lens[st.query_docs], cfg.tq, cfg.prefix_len, cfg.doc_stored_start,
+                         st.n_store_tokens)
+    dev = {k: pl.to_device(t[k], g.dtype) for k in ("q", "k_self", "v_self")}
+    out = torch.empty_like(dev["q"])
+    pb.allocate_initial()
+    pb.attention_q4(dev["q"], dev["k_self"], dev["v_self"], layer, out)
+    pb.prune(cfg.keep)
+    pb.advance()
+    torch.cuda.synchronize()
+    assert pb.flags() == 0
+    assert set(st.planted[0].tolist()) <= set(pb.keep_idx[0, :cfg.keep].tolist()) | set(pb.cand[0, :cfg.keep].tolist())
+    first = out.clone()
+    pb.attention_q4(dev["q"], dev["k_self"], dev["v_self"], layer, out)      # the next layer, over the survivors
+    torch.cuda.synchronize()
+    assert pb.flags() == 0 and not torch.equal(first, out) and bool(torch.isfinite(out.float()).all())
+    assert pb.mass[0, :5].sum().item() == pytest.approx(g.n_q_heads * cfg.tq, rel=1e-5)
