@@ -11,9 +11,11 @@
 // are fp32.  Tiles with a scale outside fp16's exponents are left to a second pass over the run in which keys meet a query of three e4m3 terms
 // and values and probabilities are bf16, the latter as value and remainder.
 //
-// Work: the rows that share a kv head (row m = t * group + head) are cut into 16-row blocks, one or two per wavefront.  A workgroup's eight wavefronts
-// own different rows, or stream different runs of the 32-token tiles where there are few rows, or both; none waits for another
-// before the end, where runs meet in LDS.  Splits (workgroups of the same rows) leave fp32 partial rows that a second kernel merges.
+// Work: the rows that share a kv head (row m = t * group + head) are cut into 16-row blocks.
+//   * One block (decode steps): attn_q4_solo_kernel, each of eight wavefronts streams a run of 32-token tiles of its own; they meet in LDS at the end.
+//   * More: attn_q4_rows_kernel, four wavefronts own one or two blocks each and share the tiles that they stage together.
+// Splits (workgroups of the same rows) leave fp32 partial rows that q4_combine_kernel merges; q4_mass_kernel reduces the (reference, sum) pairs
+// that the wavefronts leave per row and segment where masses are wanted.
 #include "cf_attn_tile.h"
 #include "cf_plan_q4.h"
 
@@ -35,17 +37,26 @@ using attn::wave_lds_order;
 
 namespace {
 
-constexpr int kThreads = kWaves * kWave;
+constexpr int kSoloThreads = kSoloWaves * kWave, kRowsThreads = kRowsWaves * kWave;
 constexpr int kVRow = 288;                           // bytes per token of a staged V tile
 constexpr int kVTile = kTile * kVRow;
 constexpr int kRowBytes = 64;                        // codes of a row
+constexpr int kQRow = 272;                           // bytes per row of queries in LDS
 constexpr float kProbLimit = attn::kProbLimit;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// run i of a list of `total` tiles owns [total*i/n, total*(i+1)/n)
-__device__ __forceinline__ int run_begin(int total, int n, int i) { return (int)((int64_t)total * i / n); }
+// run i of a list of `total` tiles owns [total*i/n, total*(i+1)/n) (n at most 512, so that shorter lists need no 64-bit division)
+__device__ __forceinline__ int run_begin(int total, int n, int i) {
+    if (total < (1 << 22)) return (int)div_exact((unsigned)(total * i), (unsigned)n);
+    return (int)((int64_t)total * i / n);
+}
+// the run that owns tile x
+__device__ __forceinline__ int run_of(int total, int n, int x) {
+    if (total < (1 << 22)) return (int)div_exact((unsigned)((x + 1) * n - 1), (unsigned)total);
+    return (int)((((int64_t)x + 1) * n - 1) / total);
+}
 
 // Walks the tiles of a run that lie in the store, or (OWN) in the own block.
 template <bool OWN>
@@ -117,7 +128,7 @@ __device__ __forceinline__ QueryPart load_query(const uint16_t* qp, bool valid, 
 }
 // Its channels 4n .. 4n + 3 of either half (a, b), turned by -delta.  cs: (cos, sin) of delta's 64 angles.
 template <int DT, int PAIRING>
-__device__ __forceinline__ void turn4(const QueryPart& q, int n, bool still, const float2* cs, int lg, float (&a)[4], float (&b)[4]) {
+__device__ __forceinline__ void turn4(const QueryPart& q, int n, const float2* cs, int lg, float (&a)[4], float (&b)[4]) {
     const uint4 wa = q.w[n >> 1], wb = q.w[2 + (n >> 1)];
     const uint32_t ua[2] = {n & 1 ? wa.z : wa.x, n & 1 ? wa.w : wa.y}, ub[2] = {n & 1 ? wb.z : wb.x, n & 1 ? wb.w : wb.y};
 #pragma unroll
@@ -125,7 +136,6 @@ __device__ __forceinline__ void turn4(const QueryPart& q, int n, bool still, con
         a[i] = i & 1 ? Mma<DT>::hi(ua[i >> 1]) : Mma<DT>::lo(ua[i >> 1]);
         b[i] = i & 1 ? Mma<DT>::hi(ub[i >> 1]) : Mma<DT>::lo(ub[i >> 1]);
     }
-    if (still) return;                               // wavefront-uniform
     if constexpr (PAIRING == CF_ROPE_HALF) {         // slice m: channels m, m + 64
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -147,55 +157,72 @@ __device__ __forceinline__ void turn4(const QueryPart& q, int n, bool still, con
     }
 }
 
-// The exponent byte of a row's power of two: its largest channel, turned by any angle, comes to at most 2^7 * sqrt(2) of it; 255 (NaN) for a
-// row that is not finite.
+// The bits of the largest magnitude among a lane's channels, but for those that are not finite.
 template <int DT>
-__device__ __forceinline__ int row_scale(const QueryPart& q) {
-    uint32_t top = 0;                                // magnitudes as bits: a NaN counts as the largest
+__device__ __forceinline__ uint32_t largest(const QueryPart& q) {
+    constexpr uint32_t kInf = DT == CF_BF16 ? 0x7f80u : 0x7c00u;
+    uint32_t top = 0;
+    auto take = [&](uint32_t x) { top = max(top, x < kInf ? x : 0u); };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t u[4] = {q.w[i].x, q.w[i].y, q.w[i].z, q.w[i].w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = max(top, max(u[j] & 0x7fffu, u[j] >> 16 & 0x7fffu));
+        for (int j = 0; j < 4; ++j) {
+            take(u[j] & 0x7fffu);
+            take(u[j] >> 16 & 0x7fffu);
+        }
     }
+    return top;
+}
+// The exponent byte of the power of two that queries are scaled down by: the largest channel, turned by any angle, comes to at most 2^7 * sqrt(2).
+template <int DT>
+__device__ __forceinline__ int scale_byte_of(uint32_t top) { return max((int)(__float_as_uint(Mma<DT>::lo(top)) >> 23) - 6, 27); }
+template <int DT>
+__device__ __forceinline__ int row_scale(const QueryPart& q) {
+    uint32_t top = largest<DT>(q);
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    if (top >= (DT == CF_BF16 ? 0x7f80u : 0x7c00u)) return 255;
-    const float t = Mma<DT>::lo(top);
-    return max((int)(__float_as_uint(t) >> 23) - 6, 27);
+    return scale_byte_of<DT>(top);
 }
 
-__device__ __forceinline__ float scale_down(int scale) { return __uint_as_float((uint32_t)(254 - min(scale, 253)) << 23); }
+__device__ __forceinline__ float scale_down(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
 
 // A 16-row block of turned queries: fp16 values (hi[s]: channels 32 lg + 8 s .. + 7) and what is left, 2^11 times larger, in e4m3.
 constexpr int kLoScale = 127 - 11;
 struct Parts { uint4 hi[4]; i32x8 lo; };
 
-// `lds`: the wavefront's staging rows.  A lane turns channels 16 lg .. and 64 + 16 lg .. (both of a slice), the fp16 fragments want 32 lg ...
+// `down`: scales the queries, if `cs` does not.
 template <int DT, int PAIRING>
-__device__ __forceinline__ Parts to_parts(const QueryPart& q, int scale, bool still, const float2* cs, unsigned char* lds, int li, int lg) {
-    const float down = scale_down(scale);
+__device__ __forceinline__ Parts to_parts(const QueryPart& q, float down, const float2* cs, int lg) {
     Parts r;
-    auto split = [&](float (&v)[4], int w, unsigned char* at) __attribute__((always_inline)) {
-        const uint32_t h0 = Mma<CF_F16>::pack(v[0] * down, v[1] * down), h1 = Mma<CF_F16>::pack(v[2] * down, v[3] * down);
-        *reinterpret_cast<uint2*>(at) = make_uint2(h0, h1);
-        auto rest = [&](int i, float h) { return fmaf(v[i], down, -h) * 2048.f; };       // exact
-        const int packed = __builtin_amdgcn_cvt_pk_fp8_f32(rest(0, Mma<CF_F16>::lo(h0)), rest(1, Mma<CF_F16>::hi(h0)), 0, false);
-        r.lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(rest(2, Mma<CF_F16>::lo(h1)), rest(3, Mma<CF_F16>::hi(h1)), packed, true);
+    uint32_t h[2][8];                                // fp16 pairs of either half
+    auto split = [&](float (&v)[4], int w, uint32_t (&h)[8], int at) __attribute__((always_inline)) {
+        h[at] = Mma<CF_F16>::pack(v[0] * down, v[1] * down);
+        h[at + 1] = Mma<CF_F16>::pack(v[2] * down, v[3] * down);
+        auto rest = [&](int i, float x) { return fmaf(v[i], down, -x) * 2048.f; };       // exact
+        const int packed = __builtin_amdgcn_cvt_pk_fp8_f32(rest(0, Mma<CF_F16>::lo(h[at])), rest(1, Mma<CF_F16>::hi(h[at])), 0, false);
+        r.lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(rest(2, Mma<CF_F16>::lo(h[at + 1])), rest(3, Mma<CF_F16>::hi(h[at + 1])), packed, true);
     };
-    unsigned char* const write = lds + li * kVRow + 32 * lg;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         float a[4], b[4];
-        turn4<DT, PAIRING>(q, n, still, cs, lg, a, b);
-        split(a, n, write + 8 * n);
-        split(b, 4 + n, write + 128 + 8 * n);
+        turn4<DT, PAIRING>(q, n, cs, lg, a, b);
+        split(a, n, h[0], 2 * n);
+        split(b, 4 + n, h[1], 2 * n);
         __builtin_amdgcn_sched_barrier(0);           // few floats at a time
     }
-    wave_lds_order();
+    // A lane has turned channels 16 lg .. and 64 + 16 lg .. (both of a slice), the fp16 fragments want 32 lg ...: lane groups 0 | 1 | 2 | 3 take the
+    // first halves of groups 0, 1 | 2, 3 and the second halves of 0, 1 | 2, 3
+    uint32_t f[16];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) r.hi[s] = *reinterpret_cast<const uint4*>(lds + li * kVRow + 64 * lg + 16 * s);
-    wave_lds_order();
+    for (int i = 0; i < 8; ++i) {
+        const auto x = __builtin_amdgcn_permlane32_swap(h[0][i], h[1][i], false, false);
+        const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
+        f[i] = y[0];
+        f[8 + i] = y[1];
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) r.hi[s] = make_uint4(f[4 * s], f[4 * s + 1], f[4 * s + 2], f[4 * s + 3]);
     return r;
 }
 
@@ -204,7 +231,7 @@ constexpr int kTerms = 3;
 struct Terms { i32x8 t[kTerms]; };
 
 template <int DT, int PAIRING>
-__device__ __forceinline__ Terms to_terms(const QueryPart& q, int scale, bool still, const float2* cs, int lg) {
+__device__ __forceinline__ Terms to_terms(const QueryPart& q, int scale, const float2* cs, int lg) {
     const float down = scale_down(scale);
     Terms r;
     auto split = [&](float (&v)[4], int w) __attribute__((always_inline)) {
@@ -227,7 +254,7 @@ __device__ __forceinline__ Terms to_terms(const QueryPart& q, int scale, bool st
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         float a[4], b[4];
-        turn4<DT, PAIRING>(q, n, still, cs, lg, a, b);
+        turn4<DT, PAIRING>(q, n, cs, lg, a, b);
         split(a, n);
         split(b, 4 + n);
         __builtin_amdgcn_sched_barrier(0);
@@ -268,127 +295,45 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo
     split2<DT>(v[6], v[7], hi.w, lo.w);
 }
 
-template <int DT, int PAIRING, int NRB, bool REG_TABLE>
-__global__ __launch_bounds__(kThreads, 2) void attn_q4_kernel(AttnArgs a, RopeFreq freq, Plan p, Scales s) {
-    __shared__ std::conditional_t<REG_TABLE, int, SegTable> tbl;
-    constexpr int kMerge = kWaves * 8 * kWave * (int)sizeof(f32x4);
-    __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * kVTile > kMerge ? kWaves * kVTile : kMerge];
-    __shared__ __attribute__((aligned(16))) float2 cs_lds[kWaves][64];
-    __shared__ float2 red_ml[kWaves][NRB * 16];
-
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int li = lane & 15, lg = lane >> 4;
-    // grid (split, kv head * row groups + row group, query)
-    const int split = blockIdx.x, b = blockIdx.z;
-    const int hkv = (int)div_exact(blockIdx.y, (unsigned)p.n_rg), rg = (int)blockIdx.y - hkv * p.n_rg;
-    const int unit = b * p.units_per_b + (int)blockIdx.y;
-    const int row_wave = wave & (p.row_waves - 1), run = (int)div_exact((unsigned)wave, (unsigned)p.row_waves);
-    const int group = p.group;
-    const QueryHead qh = load_query_head(a, b, REG_TABLE ? lane : (int)threadIdx.x);
-    const double my_freq = freq.rev[lane];
-    const int tq = max(min(qh.tq_raw, a.max_tq), 0);
-    const int n_rows = group * tq;
-    const int row0 = rg * p.rows_wg + row_wave * NRB * 16;       // the wavefront's first row
-
-    RegSegTable rtbl;
-    int total;
-    if constexpr (REG_TABLE) {
-        rtbl = build_reg_table(a, qh, lane, kTile);
-        total = rtbl.total;
-    } else {
-        build_table(a, qh, &tbl, kTile);
-        total = tbl.tile0[tbl.n];
-    }
-    const int nsub = p.nsplit * p.runs, ss = split * p.runs + run;
-    const bool has_rows = row0 < n_rows;             // wavefront-uniform
-    const int t_begin = run_begin(total, nsub, ss), t_end = has_rows ? run_begin(total, nsub, ss + 1) : 0;
-    RunWalk<false> walk(t_begin, t_end);
-
-    // row m = t * group + head
-    int trow[NRB], qrow[NRB];                        // place in the own block (-1: no row); row of q and out, counted from the query's first
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-        const int m = row0 + 16 * rb + li;
-        const bool valid = m < n_rows;
-        const int t = valid ? (int)div_exact((unsigned)m, (unsigned)group) : 0, g = valid ? m - t * group : 0;
-        trow[rb] = valid ? t : -1;
-        qrow[rb] = t * a.n_q_heads + hkv * group + g;
-    }
-    const int64_t q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
-    auto query = [&](int rb) {
-        int row = qrow[rb];
-        asm volatile("" : "+v"(row));                // its addresses are worked out anew, not kept through the loops
-        return load_query(static_cast<const uint16_t*>(a.q) + q_first + (int64_t)row * kD, trow[rb] >= 0, lg);
-    };
-
-    int q_scale[NRB];
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) q_scale[rb] = row_scale<DT>(query(rb));
-
-    // One tile's codes and scales: token 16 tb + li, 32 channels from 32 lg on.
-    struct Regs { i32x4 k[2], v[2]; uint32_t ks[2], vs[2]; };
-    const int row_bytes = (int)(a.store_ts >> 1), scale_bytes = (int)(a.store_ts >> 5);
-    auto fetch = [&](RunWalk<false>& walk, Tile& d, Regs& r) {
-        if constexpr (REG_TABLE) d = walk.next(rtbl, lane);
-        else d = walk.next(tbl, lane);
-        // rows past a ragged tile's end, and everything where no tile of the store is left, lie past the range and read as zero
-        const bool any = d.ntok > 0;
-        const int64_t at = any ? (walk.c_tok + d.tok0) * a.store_ts + (int64_t)hkv * a.store_hs : 0;
-        const int codes = any ? (d.ntok - 1) * row_bytes + kRowBytes : 0, scales = any ? (d.ntok - 1) * scale_bytes + 4 : 0;
-        auto rsrc = [](const void* base, int64_t off, int range) {
-            return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + off), 0, range, 0x00020000);
-        };
-        const auto rk = rsrc(a.k_store, at >> 1, codes), rv = rsrc(a.v_store, at >> 1, codes);
-        const auto sk = rsrc(s.k, at >> 5, scales), sv = rsrc(s.v, at >> 5, scales);
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb) {
-            const int off = (16 * tb + li) * row_bytes + 16 * lg, soff = (16 * tb + li) * scale_bytes + lg;
-            r.k[tb] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
-            r.v[tb] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
-            r.ks[tb] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sk, soff, 0, 0);
-            r.vs[tb] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sv, soff, 0, 0);
-        }
-    };
-
+// ---------------------------------------------------------------------------------------------
+// What a wavefront accumulates for its NRB 16-row blocks, and what it needs to go on: lane (li, lg) holds, for row li of each block, the output
+// channels 16 db + 4 lg + r, the reference maximum and the sums over the tokens that it has seen (whole call and current segment).
+template <int NRB>
+struct Rows {
     f32x4 acc[NRB][8];
     float m_run[NRB], l_run[NRB], seg_l[NRB];
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-#pragma unroll
-        for (int db = 0; db < 8; ++db) acc[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-        m_run[rb] = -INFINITY;
-        l_run[rb] = seg_l[rb] = 0.f;
-    }
-    char* const ws = static_cast<char*>(a.workspace);
-    float2* const massml = reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * p.rows_wg + row_wave * NRB * 16;
-    const bool want_mass = a.mass != nullptr;
-    // what scores are multiplied by: of whole queries, and of those scaled down by their row's power of two
-    const float scale_log2e = a.scale_log2e;
-    auto plain_mul = [&](int) { return scale_log2e; };
-    auto part_mul = [&](int rb) { return scale_log2e * scale_of((uint32_t)q_scale[rb]); };
-    unsigned char* const v_lds = lds + wave * kVTile;
-    unsigned char* const v_write = v_lds + li * kVRow + 64 * lg;
-    const unsigned char* const v_read = v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
+    int trow[NRB], qrow[NRB];   // place in the own block (-1: no row); row of q and out, counted from the query's first
+    int cur_seg;
 
-    // (reference, sum) per row of the segment that ends here; `again`: added to what its slot holds, whose reference is not larger
-    bool again = false;
-    auto emit = [&](int seg) {
+    // the rows from `row0` on of kv head `hkv`, of which the query has n_rows
+    __device__ __forceinline__ void begin(int row0, int n_rows, int group, int n_q_heads, int hkv, int li) {
+        cur_seg = -1;
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
-            float tot = seg_l[rb] + __shfl_xor(seg_l[rb], 16);
-            tot += __shfl_xor(tot, 32);
-            if (lg == 0) {
-                float2* slot = massml + (int64_t)(seg + ss) * p.rows_wg + 16 * rb + li;
-                if (again && slot->x != -INFINITY) tot += slot->y * __builtin_amdgcn_exp2f(slot->x - m_run[rb]);
-                *slot = make_float2(m_run[rb], tot);
-            }
+#pragma unroll
+            for (int db = 0; db < 8; ++db) acc[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m_run[rb] = -INFINITY;
+            l_run[rb] = seg_l[rb] = 0.f;
+            const int m = row0 + 16 * rb + li;
+            const bool valid = m < n_rows;
+            const int t = valid ? (int)div_exact((unsigned)m, (unsigned)group) : 0, g = valid ? m - t * group : 0;
+            trow[rb] = valid ? t : -1;
+            qrow[rb] = t * n_q_heads + hkv * group + g;
         }
-    };
-    // Online softmax (exp2 domain) of scores sc, in units of `mul` per row, against a stale row maximum: probabilities pv; see kProbLimit.
-    auto softmax = [&](f32x4 (&sc)[NRB][2], auto mul, float (&pv)[NRB][8]) {
+    }
+    // One place for the accumulators: across a branch that scales them the compiler would otherwise keep a copy for either way (at two
+    // row blocks that spilled 200 bytes a lane).
+    __device__ __forceinline__ void pin() {
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+            for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(acc[rb][db]));
+    }
+    // Online softmax (exp2 domain) of scores sc, in units of mul(block), against a stale row maximum: probabilities pv; see kProbLimit.
+    template <class F>
+    __device__ __forceinline__ void softmax(f32x4 (&sc)[NRB][2], F mul, float (&pv)[NRB][8]) {
         float lsum[NRB];
-        auto probabilities = [&](int rb) {
+        auto probabilities = [&](int rb) __attribute__((always_inline)) {
             const float m_safe = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
             lsum[rb] = 0.f;
 #pragma unroll
@@ -422,381 +367,682 @@ __global__ __launch_bounds__(kThreads, 2) void attn_q4_kernel(AttnArgs a, RopeFr
                 probabilities(rb);
             }
         }
-        // (one place for the accumulators: the compiler would keep a copy for either way through the branch)
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-            for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(acc[rb][db]));
+        pin();
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
             l_run[rb] += lsum[rb];
             seg_l[rb] += lsum[rb];
         }
-    };
-    // O^T += V^T P^T; VT: the type V is staged in.  `exact`: P as value and remainder.
-    auto weigh = [&](auto vt, auto exact, const float (&pv)[NRB][8]) {
-        constexpr int VT = decltype(vt)::value;
+    }
+    // O^T += V^T P^T, V staged in the type VT.  EXACT: P as value and remainder.
+    template <int VT, bool EXACT>
+    __device__ __forceinline__ void weigh(const unsigned char* v_read, const float (&pv)[NRB][8]) {
         uint4 ph[NRB], pl[NRB];
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) split8<VT>(pv[rb], ph[rb], pl[rb]);
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
-            if (NRB > 1 && (db & 3) == 0) __builtin_amdgcn_sched_barrier(0);     // half of V^T in registers
             const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(v_read + 32 * db));
             const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(v_read + 32 * db + 16 * kVRow));
             const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
             const uint4 va = make_uint4(l2.x, l2.y, h2.x, h2.y);
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) {
-                if constexpr (decltype(exact)::value) acc[rb][db] = Mma<VT>::run(va, pl[rb], acc[rb][db]);
+                if constexpr (EXACT) acc[rb][db] = Mma<VT>::run(va, pl[rb], acc[rb][db]);
                 acc[rb][db] = Mma<VT>::run(va, ph[rb], acc[rb][db]);
             }
         }
-    };
-
-    int cs_delta = 0, cur_seg = -1;
-    auto angles = [&](int delta) {                   // the wavefront's table of (cos, sin)
-        if (delta == 0 || delta == cs_delta) return;
-        cs_delta = delta;
-        wave_lds_order();
-        cs_lds[wave][lane] = rope_cos_sin_fast(delta, my_freq);
-        wave_lds_order();
-    };
-    auto enter = [&](int seg) {
+    }
+    // (reference, sum) per row of the segment that ends here, to its slot; `again`: added to what the slot holds, whose reference is not larger
+    __device__ __forceinline__ void emit(float2* massml, int rows_wg, int ss, bool again, int li, int lg) {
+        if (cur_seg < 0 || massml == nullptr) return;
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            float tot = seg_l[rb] + __shfl_xor(seg_l[rb], 16);
+            tot += __shfl_xor(tot, 32);
+            if (lg == 0) {
+                float2* slot = massml + (int64_t)(cur_seg + ss) * rows_wg + 16 * rb + li;
+                if (again && slot->x != -INFINITY) tot += slot->y * __builtin_amdgcn_exp2f(slot->x - m_run[rb]);
+                *slot = make_float2(m_run[rb], tot);
+            }
+        }
+    }
+    __device__ __forceinline__ void enter(int seg, float2* massml, int rows_wg, int ss, bool again, int li, int lg) {
         if (seg == cur_seg) return;
-        if (want_mass && cur_seg >= 0) emit(cur_seg);
+        emit(massml, rows_wg, ss, again, li, lg);
         cur_seg = seg;
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) seg_l[rb] = 0.f;
-    };
+    }
+    // row sums over the four lane groups
+    __device__ __forceinline__ void close() {
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            l_run[rb] += __shfl_xor(l_run[rb], 16);
+            l_run[rb] += __shfl_xor(l_run[rb], 32);
+        }
+    }
+};
 
-    // ---- the run's tiles of the store.  `wide` false: those whose values fit fp16, the others are passed over; true: the others, with values and
-    // probabilities in bf16 (the latter as value and remainder).
-    bool passed_over = false;
-    auto store_tiles = [&](auto wide, RunWalk<false>& walk, Tile d, Regs& r) {
-        constexpr int VT = decltype(wide)::value ? CF_BF16 : CF_F16;
-        std::conditional_t<decltype(wide)::value, Terms, Parts> qt[NRB];
-        int q_delta = 0;
-        bool have_terms = false;
-        while (d.ntok > 0) {
-            const Tile cd = d;
-            const bool fits = __all(((fits_f16(r.ks[0]) && fits_f16(r.vs[0])) || li >= cd.ntok) &&
-                                    ((fits_f16(r.ks[1]) && fits_f16(r.vs[1])) || 16 + li >= cd.ntok));
-            // a tile that is passed over counts as one without tokens (no branch around the body: the compiler would keep the accumulators twice)
-            const bool take = fits != decltype(wide)::value;
-            const int ntok = take ? cd.ntok : 0;
-            passed_over = passed_over || !take;
-            enter(cd.seg);
-            if (!have_terms || cd.delta != q_delta) {
-                have_terms = true;
-                q_delta = cd.delta;
-                angles(cd.delta);
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) {
-                    const QueryPart q = query(rb);
-                    if constexpr (decltype(wide)::value) qt[rb] = to_terms<DT, PAIRING>(q, q_scale[rb], cd.delta == 0, cs_lds[wave], lg);
-                    else qt[rb] = to_parts<DT, PAIRING>(q, q_scale[rb], cd.delta == 0, cs_lds[wave], v_lds, li, lg);
-                }
-            }
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    *reinterpret_cast<uint4*>(v_write + 16 * tb * kVRow + 16 * c) = unpack8<VT>(r.v[tb][c], take ? scale_of(r.vs[tb]) : 0.f);
-            wave_lds_order();
-            f32x4 sc[NRB][2];
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if constexpr (decltype(wide)::value) {
-#pragma unroll
-                for (int k = kTerms - 1; k >= 0; --k)        // the smallest terms first
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                        for (int tb = 0; tb < 2; ++tb)
-                            sc[rb][tb] = mma_fp4(r.k[tb], (int)r.ks[tb], qt[rb].t[k], q_scale[rb] == 255 ? 255 : q_scale[rb] - 4 * k, sc[rb][tb]);
-            } else {
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) sc[rb][tb] = mma_fp4(r.k[tb], (int)r.ks[tb], qt[rb].lo, kLoScale, sc[rb][tb]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        const uint4 kf = unpack8<CF_F16>(r.k[tb][c], take ? scale_of(r.ks[tb]) : 0.f);
-#pragma unroll
-                        for (int rb = 0; rb < NRB; ++rb) sc[rb][tb] = Mma<CF_F16>::run(kf, qt[rb].hi[c], sc[rb][tb]);
-                    }
-            }
-            fetch(walk, d, r);                       // the registers are free again
-            if (ntok < kTile) {
-                const int lim = ntok - 4 * lg;
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
-            }
-            float pv[NRB][8];
-            if constexpr (decltype(wide)::value) softmax(sc, plain_mul, pv);
-            else softmax(sc, part_mul, pv);
-            weigh(std::integral_constant<int, VT>{}, wide, pv);
-            wave_lds_order();                        // the next step writes over what others read above
-        }
-    };
-    {
-        Tile d;
-        Regs r;
-        fetch(walk, d, r);
-        store_tiles(std::false_type{}, walk, d, r);
-    }
-    const bool own_tiles = walk.others;
-    if (passed_over) {
-        if (want_mass && cur_seg >= 0) emit(cur_seg);
-        cur_seg = -1;
-        again = true;                                // the segments' slots hold sums already
-        RunWalk<false> rest(t_begin, t_end);
-        Tile d;
-        Regs r;
-        fetch(rest, d, r);
-        store_tiles(std::true_type{}, rest, d, r);
-        if (want_mass && cur_seg >= 0) emit(cur_seg);
-        cur_seg = -1;
-        again = false;
-    }
-    // ---- its tiles of the own block: 16-bit keys and values, row t sees tokens 0 .. t
-    if (own_tiles) {
-        RunWalk<true> own(t_begin, t_end);
-        for (;;) {
-            Tile cd;
-            if constexpr (REG_TABLE) cd = own.next(rtbl, lane);
-            else cd = own.next(tbl, lane);
-            if (cd.ntok <= 0) break;
-            enter(cd.seg);
-            angles(cd.delta);
-            const int64_t at = ((own.c_tok + cd.tok0) * a.n_kv_heads + hkv) * kD * 2;
-            const int pitch = a.n_kv_heads * kD * 2, range = (cd.ntok - 1) * pitch + 2 * kD;
-            const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(a.k_self) + at), 0, range, 0x00020000);
-            const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(a.v_self) + at), 0, range, 0x00020000);
-            uint4 kf[2][4];
-            uint32_t odd = 0;                        // tokens with values that are not finite
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-                bool any = false;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    kf[tb][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, (16 * tb + li) * pitch + 32 * lg + 128 * (c >> 1) + 16 * (c & 1), 0, 0));
-                    const uint4 v = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, (16 * tb + li) * pitch + 64 * lg + 16 * c, 0, 0));
-                    *reinterpret_cast<uint4*>(v_write + 16 * tb * kVRow + 16 * c) = finite8<DT>(v, any);
-                }
-                const uint64_t at = __ballot(any);
-                odd |= (uint32_t)((at | at >> 16 | at >> 32 | at >> 48) & 0xffff) << (16 * tb);
-            }
-            wave_lds_order();
-            f32x4 sc[NRB][2];
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) {
-                const QueryPart q = query(rb);
-                sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {        // channels 8c .. 8c + 7 of either half
-                    float a0[4], b0[4], a1[4], b1[4];
-                    turn4<DT, PAIRING>(q, 2 * c, cd.delta == 0, cs_lds[wave], lg, a0, b0);
-                    turn4<DT, PAIRING>(q, 2 * c + 1, cd.delta == 0, cs_lds[wave], lg, a1, b1);
-                    const float va[8] = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
-                    const float vb[8] = {b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
-                    uint4 ha, la, hb, lb;
-                    split8<DT>(va, ha, la);
-                    split8<DT>(vb, hb, lb);
-#pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        sc[rb][tb] = Mma<DT>::run(kf[tb][c], la, sc[rb][tb]);
-                        sc[rb][tb] = Mma<DT>::run(kf[tb][2 + c], lb, sc[rb][tb]);
-                        sc[rb][tb] = Mma<DT>::run(kf[tb][c], ha, sc[rb][tb]);
-                        sc[rb][tb] = Mma<DT>::run(kf[tb][2 + c], hb, sc[rb][tb]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                const int last = min(cd.ntok - 1, trow[rb] - cd.tok0) - 4 * lg;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) <= last ? sc[rb][e >> 2][e & 3] : -INFINITY;
-            }
-            float pv[NRB][8];
-            softmax(sc, plain_mul, pv);
-            weigh(std::integral_constant<int, DT>{}, std::true_type{}, pv);
-            wave_lds_order();                        // the next tile writes over what others read above
-            // values that are not finite, for the rows that see them (zero times one would reach the rows ahead)
-            for (; odd; odd &= odd - 1) {
-                const int j = __builtin_ctz(odd);
-#pragma unroll
-                for (int db = 0; db < 8; ++db) {
-                    const auto w = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rv, j * pitch + 32 * db + 8 * lg, 0, 0));
-                    const float v[4] = {Mma<DT>::lo(w.x), Mma<DT>::hi(w.x), Mma<DT>::lo(w.y), Mma<DT>::hi(w.y)};
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (cd.tok0 + j <= trow[rb] && !(fabsf(v[r]) < INFINITY)) acc[rb][db][r] += v[r];
-                }
-            }
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(acc[rb][db]));
-        }
-    }
-    if (want_mass && cur_seg >= 0) emit(cur_seg);
-
-    // ---- the runs of the same rows meet: wavefront `run` takes the channel blocks run, run + runs, ...
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-        l_run[rb] += __shfl_xor(l_run[rb], 16);
-        l_run[rb] += __shfl_xor(l_run[rb], 32);
-        if (lg == 0) red_ml[wave][16 * rb + li] = make_float2(m_run[rb], l_run[rb]);
-    }
-    f32x4* const red = reinterpret_cast<f32x4*>(lds);
-    const int64_t part = (int64_t)unit * p.nsplit + split;
-    float2* const ml = reinterpret_cast<float2*>(ws + p.off_ml) + part * p.rows_wg + row_wave * NRB * 16;
-    float* const opart = reinterpret_cast<float*>(ws + p.off_opart) + (part * p.rows_wg + row_wave * NRB * 16) * kD;
-    auto meet = [&](auto block) {
-        constexpr int rb = decltype(block)::value;
-        __syncthreads();                             // nobody reads a V tile, or the block before, any more
-#pragma unroll
-        for (int db = 0; db < 8; ++db) red[(wave * 8 + db) * kWave + lane] = acc[rb][db];
-        __syncthreads();
-        float m = -INFINITY;
-        for (int w = 0; w < p.runs; ++w) m = fmaxf(m, red_ml[w * p.row_waves + row_wave][16 * rb + li].x);
-        const float ms = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        for (int w = 0; w < p.runs; ++w) {
-            const float2 x = red_ml[w * p.row_waves + row_wave][16 * rb + li];
-            l += x.y * __builtin_amdgcn_exp2f(x.x - ms);
-        }
-        const float inv = l > 0.f ? 1.f / l : l;     // (a sum that is not a number stays one)
-        if (run == 0 && lg == 0) ml[16 * rb + li] = make_float2(m, trow[rb] >= 0 ? l : 0.f);
-        for (int db = run; db < 8; db += p.runs) {
-            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int w = 0; w < p.runs; ++w) {
-                const int from = w * p.row_waves + row_wave;
-                o += red[(from * 8 + db) * kWave + lane] * __builtin_amdgcn_exp2f(red_ml[from][16 * rb + li].x - ms);
-            }
-            o *= inv;
-            if (p.direct_out) {
-                if (trow[rb] >= 0) {
-                    uint16_t* op = static_cast<uint16_t*>(a.out) + q_first + (int64_t)qrow[rb] * kD + 16 * db + 4 * lg;
-                    *reinterpret_cast<uint2*>(op) = make_uint2(Mma<DT>::pack(o[0], o[1]), Mma<DT>::pack(o[2], o[3]));
-                }
-            } else {
-                *reinterpret_cast<f32x4*>(opart + (16 * rb + li) * kD + 16 * db + 4 * lg) = o;
-            }
-        }
-    };
-    meet(std::integral_constant<int, 0>{});
-    if constexpr (NRB > 1) meet(std::integral_constant<int, 1>{});
+// A buffer of `range` bytes from base + off on; reads past it give zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* base, int64_t off, int range) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + off), 0, range, 0x00020000);
 }
 
-// Merges the splits' partial rows: half a wavefront per row, four channels per lane.
-template <int DT>
-__global__ __launch_bounds__(256) void q4_combine_kernel(AttnArgs a, Plan p) {
-    const int b = blockIdx.z, unit = b * p.units_per_b + (int)blockIdx.y;
-    const int hkv = (int)div_exact(blockIdx.y, (unsigned)p.n_rg), rg = (int)blockIdx.y - hkv * p.n_rg;
-    const int row = (int)blockIdx.x * 8 + (int)threadIdx.x / 32, c = 4 * (threadIdx.x & 31);
-    const int tq = max(min(a.q_off[b + 1] - a.q_off[b], a.max_tq), 0);
-    const int m2 = rg * p.rows_wg + row;
-    if (row >= p.rows_wg || m2 >= p.group * tq) return;
-    const char* ws = static_cast<const char*>(a.workspace);
-    const int64_t first = (int64_t)unit * p.nsplit * p.rows_wg + row;
-    const float2* ml = reinterpret_cast<const float2*>(ws + p.off_ml) + first;
-    const float* opart = reinterpret_cast<const float*>(ws + p.off_opart) + first * kD + c;
-    float m = -INFINITY;
-    for (int s = 0; s < p.nsplit; ++s) m = fmaxf(m, ml[(int64_t)s * p.rows_wg].x);
-    m = m == -INFINITY ? 0.f : m;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    for (int s = 0; s < p.nsplit; ++s) {
-        const float2 x = ml[(int64_t)s * p.rows_wg];
-        const float w = x.y * __builtin_amdgcn_exp2f(x.x - m);
-        l += w;
-        o += *reinterpret_cast<const f32x4*>(opart + (int64_t)s * p.rows_wg * kD) * w;
+// A tile of the store for a wavefront on its own: token 16 tb + li, 32 channels from 32 lg on.
+struct TileRegs { i32x4 k[2], v[2]; uint32_t ks[2], vs[2]; };
+__device__ __forceinline__ void load_tile(const AttnArgs& a, const Scales& s, const Tile& d, int64_t seg_tok, int hkv, int li, int lg, TileRegs& r) {
+    const int row_bytes = (int)(a.store_ts >> 1), scale_bytes = (int)(a.store_ts >> 5);
+    // rows past a ragged tile's end, and everything where no tile is left, lie past the range and read as zero
+    const bool any = d.ntok > 0;
+    const int64_t at = any ? (seg_tok + d.tok0) * a.store_ts + (int64_t)hkv * a.store_hs : 0;
+    const int codes = any ? (d.ntok - 1) * row_bytes + kRowBytes : 0, scales = any ? (d.ntok - 1) * scale_bytes + 4 : 0;
+    const auto rk = buffer(a.k_store, at >> 1, codes), rv = buffer(a.v_store, at >> 1, codes);
+    const auto sk = buffer(s.k, at >> 5, scales), sv = buffer(s.v, at >> 5, scales);
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+        const int off = (16 * tb + li) * row_bytes + 16 * lg, soff = (16 * tb + li) * scale_bytes + lg;
+        r.k[tb] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
+        r.v[tb] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
+        r.ks[tb] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sk, soff, 0, 0);
+        r.vs[tb] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sv, soff, 0, 0);
     }
-    o *= l > 0.f ? 1.f / l : l;
-    const int t = (int)div_exact((unsigned)m2, (unsigned)p.group), g = m2 - t * p.group;
-    uint16_t* op = static_cast<uint16_t*>(a.out) + (((int64_t)a.q_off[b] + t) * a.n_q_heads + hkv * p.group + g) * kD + c;
+}
+__device__ __forceinline__ bool tile_fits(const TileRegs& r, int ntok, int li) {
+    return __all(((fits_f16(r.ks[0]) && fits_f16(r.vs[0])) || li >= ntok) && ((fits_f16(r.ks[1]) && fits_f16(r.vs[1])) || 16 + li >= ntok));
+}
+
+// What the passes of a wavefront on its own need of the kernel around them.
+struct WavePlace {
+    int li, lg, hkv, rows_wg, ss;
+    int t_begin, t_end;         // its run of tiles
+    int64_t q_first;            // the query's first row in q and out, in elements
+    double my_freq;             // of slice `lane`
+    float2* cs;                 // 64 entries of LDS
+    unsigned char* v_lds;       // kVTile bytes of LDS
+    float2* massml;             // slots of its rows, or NULL
+};
+
+// cos and sin of delta's 64 angles to LDS, times `down`
+__device__ __forceinline__ void put_angles(float2* cs, int lane, int delta, double my_freq, float down) {
+    wave_lds_order();
+    const float2 c = rope_cos_sin_fast(delta, my_freq);
+    cs[lane] = make_float2(c.x * down, c.y * down);
+    wave_lds_order();
+}
+
+template <int NRB>
+__device__ __forceinline__ QueryPart query_part(const AttnArgs& a, const WavePlace& w, const Rows<NRB>& st, int rb) {
+    int row = st.qrow[rb];
+    asm volatile("" : "+v"(row));                    // its addresses are worked out anew, not kept through the loops
+    return load_query(static_cast<const uint16_t*>(a.q) + w.q_first + (int64_t)row * kD, st.trow[rb] >= 0, w.lg);
+}
+
+// The second pass over a run: the tiles whose scales do not fit fp16, with keys as codes, the query in three e4m3 terms and values and
+// probabilities in bf16, the latter as value and remainder.  The segments' slots hold sums already.
+template <int DT, int PAIRING, int NRB, class Table>
+__device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, const Table& tbl, const WavePlace& w, Rows<NRB>& st) {
+    st.emit(w.massml, w.rows_wg, w.ss, false, w.li, w.lg);
+    st.cur_seg = -1;
+    const int lane = 16 * w.lg + w.li;
+    RunWalk<false> walk(w.t_begin, w.t_end);
+    for (;;) {
+        const Tile d = walk.next(tbl, lane);
+        if (d.ntok <= 0) break;
+        TileRegs r;
+        load_tile(a, s, d, walk.c_tok, w.hkv, w.li, w.lg, r);
+        if (tile_fits(r, d.ntok, w.li)) continue;
+        st.enter(d.seg, w.massml, w.rows_wg, w.ss, true, w.li, w.lg);
+        put_angles(w.cs, lane, d.delta, w.my_freq, 1.f);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *reinterpret_cast<uint4*>(w.v_lds + (16 * tb + w.li) * kVRow + 64 * w.lg + 16 * c) = unpack8<CF_BF16>(r.v[tb][c], scale_of(r.vs[tb]));
+        wave_lds_order();
+        f32x4 sc[NRB][2];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            const QueryPart q = query_part(a, w, st, rb);
+            const int scale = row_scale<DT>(q);
+            const Terms qt = to_terms<DT, PAIRING>(q, scale, w.cs, w.lg);
+            sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = kTerms - 1; k >= 0; --k)    // the smallest terms first
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) sc[rb][tb] = mma_fp4(r.k[tb], (int)r.ks[tb], qt.t[k], scale - 4 * k, sc[rb][tb]);
+            const int lim = d.ntok - 4 * w.lg;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
+        }
+        float pv[NRB][8];
+        st.softmax(sc, [&](int) { return a.scale_log2e; }, pv);
+        st.template weigh<CF_BF16, true>(w.v_lds + (4 * w.lg + (w.li >> 2)) * kVRow + 8 * (w.li & 3), pv);
+        wave_lds_order();                            // the next tile writes over what others read above
+    }
+    st.emit(w.massml, w.rows_wg, w.ss, true, w.li, w.lg);
+    st.cur_seg = -1;
+}
+
+// The run's tiles of the own block: 16-bit keys and values, queries and probabilities as value and remainder; row t sees tokens 0 .. t.
+template <int DT, int PAIRING, int NRB, class Table>
+__device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, const WavePlace& w, Rows<NRB>& st) {
+    const int lane = 16 * w.lg + w.li, li = w.li, lg = w.lg;
+    RunWalk<true> walk(w.t_begin, w.t_end);
+    for (;;) {
+        const Tile cd = walk.next(tbl, lane);
+        if (cd.ntok <= 0) break;
+        st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
+        put_angles(w.cs, lane, cd.delta, w.my_freq, 1.f);
+        const int64_t at = ((walk.c_tok + cd.tok0) * a.n_kv_heads + w.hkv) * kD * 2;
+        const int pitch = a.n_kv_heads * kD * 2, range = (cd.ntok - 1) * pitch + 2 * kD;
+        const auto rk = buffer(a.k_self, at, range), rv = buffer(a.v_self, at, range);
+        uint4 kf[2][4];
+        uint32_t odd = 0;                            // tokens with values that are not finite
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+            bool any = false;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                kf[tb][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, (16 * tb + li) * pitch + 32 * lg + 128 * (c >> 1) + 16 * (c & 1), 0, 0));
+                const uint4 v = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, (16 * tb + li) * pitch + 64 * lg + 16 * c, 0, 0));
+                *reinterpret_cast<uint4*>(w.v_lds + (16 * tb + li) * kVRow + 64 * lg + 16 * c) = finite8<DT>(v, any);
+            }
+            const uint64_t ballot = __ballot(any);
+            odd |= (uint32_t)((ballot | ballot >> 16 | ballot >> 32 | ballot >> 48) & 0xffff) << (16 * tb);
+        }
+        wave_lds_order();
+        f32x4 sc[NRB][2];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            const QueryPart q = query_part(a, w, st, rb);
+            sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {            // channels 8c .. 8c + 7 of either half
+                float a0[4], b0[4], a1[4], b1[4];
+                turn4<DT, PAIRING>(q, 2 * c, w.cs, lg, a0, b0);
+                turn4<DT, PAIRING>(q, 2 * c + 1, w.cs, lg, a1, b1);
+                const float va[8] = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+                const float vb[8] = {b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
+                uint4 ha, la, hb, lb;
+                split8<DT>(va, ha, la);
+                split8<DT>(vb, hb, lb);
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) {
+                    sc[rb][tb] = Mma<DT>::run(kf[tb][c], la, sc[rb][tb]);
+                    sc[rb][tb] = Mma<DT>::run(kf[tb][2 + c], lb, sc[rb][tb]);
+                    sc[rb][tb] = Mma<DT>::run(kf[tb][c], ha, sc[rb][tb]);
+                    sc[rb][tb] = Mma<DT>::run(kf[tb][2 + c], hb, sc[rb][tb]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const int last = min(cd.ntok - 1, st.trow[rb] - cd.tok0) - 4 * lg;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) <= last ? sc[rb][e >> 2][e & 3] : -INFINITY;
+        }
+        float pv[NRB][8];
+        st.softmax(sc, [&](int) { return a.scale_log2e; }, pv);
+        st.template weigh<DT, true>(w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3), pv);
+        wave_lds_order();                            // the next tile writes over what others read above
+        // values that are not finite, for the rows that see them (zero times one would reach the rows ahead)
+        for (; odd; odd &= odd - 1) {
+            const int j = __builtin_ctz(odd);
+#pragma unroll
+            for (int db = 0; db < 8; ++db) {
+                const auto x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rv, j * pitch + 32 * db + 8 * lg, 0, 0));
+                const float v[4] = {Mma<DT>::lo(x.x), Mma<DT>::hi(x.x), Mma<DT>::lo(x.y), Mma<DT>::hi(x.y)};
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (cd.tok0 + j <= st.trow[rb] && !(fabsf(v[r]) < INFINITY)) st.acc[rb][db][r] += v[r];
+            }
+        }
+        st.pin();
+    }
+}
+
+// Normalised output channels 16 db + 4 lg .. of a lane's row to `out`, or to the split's partial rows.
+template <int DT>
+__device__ __forceinline__ void store_out(const AttnArgs& a, int64_t q_first, int qrow, int db, int lg, f32x4 o) {
+    uint16_t* op = static_cast<uint16_t*>(a.out) + q_first + (int64_t)qrow * kD + 16 * db + 4 * lg;
     *reinterpret_cast<uint2*>(op) = make_uint2(Mma<DT>::pack(o[0], o[1]), Mma<DT>::pack(o[2], o[3]));
 }
 
-// Per (unit, slot): sum over the unit's rows of sum * exp2(max - row max) / row sum.  Slots that no run wrote hold anything and are not read later.
-__global__ __launch_bounds__(256) void q4_slots_kernel(AttnArgs a, Plan p) {
-    __shared__ float2 stat[16 * 2 * kWaves];         // (row max, 1 / row sum)
-    const int unit = blockIdx.x;
-    const int b = (int)div_exact((unsigned)unit, (unsigned)p.units_per_b);
-    const int rg = (unit - b * p.units_per_b) % p.n_rg;
-    const int tq = max(min(a.q_off[b + 1] - a.q_off[b], a.max_tq), 0);
-    const int rows = min(p.rows_wg, p.group * tq - rg * p.rows_wg);
-    char* ws = static_cast<char*>(a.workspace);
-    const float2* ml = reinterpret_cast<const float2*>(ws + p.off_ml) + (int64_t)unit * p.nsplit * p.rows_wg;
-    for (int row = threadIdx.x; row < rows; row += 256) {
-        float m = -INFINITY, l = 0.f;
-        for (int s = 0; s < p.nsplit; ++s) m = fmaxf(m, ml[s * p.rows_wg + row].x);
-        m = m == -INFINITY ? 0.f : m;
-        for (int s = 0; s < p.nsplit; ++s) l += ml[s * p.rows_wg + row].y * __builtin_amdgcn_exp2f(ml[s * p.rows_wg + row].x - m);
-        stat[row] = make_float2(m, l > 0.f ? 1.f / l : l);
+// ---------------------------------------------------------------------------------------------
+// One row block (a decode step: one row per query head of a group): bound by HBM where there are enough tokens.  A wavefront's loads are two
+// tiles ahead in registers; a tile's codes meet the query in registers, its values pass through LDS of the wavefront's own.
+template <int DT, int PAIRING, bool REG_TABLE>
+__global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs a, RopeFreq freq, Plan p, Scales s) {
+    __shared__ std::conditional_t<REG_TABLE, int, SegTable> lds_tbl;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[kSoloWaves * kVTile];
+    __shared__ __attribute__((aligned(16))) float2 cs_lds[kSoloWaves][64];
+    __shared__ float2 red_ml[kSoloWaves][16];
+    static_assert(kSoloWaves * kVTile >= kSoloWaves * 8 * kWave * (int)sizeof(f32x4), "the results reuse the V tiles");
+
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int li = lane & 15, lg = lane >> 4;
+    // grid (split, kv head, query)
+    const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
+    const int unit = b * p.units_per_b + hkv;
+    const QueryHead qh = load_query_head(a, b, REG_TABLE ? lane : (int)threadIdx.x);
+    const int tq = max(min(qh.tq_raw, a.max_tq), 0);
+    Rows<1> st;
+    st.begin(0, p.group * tq, p.group, a.n_q_heads, hkv, li);
+    RegSegTable rtbl;
+    int total;
+    if constexpr (REG_TABLE) {
+        rtbl = build_reg_table(a, qh, lane, kTile);
+        total = rtbl.total;
+    } else {
+        build_table(a, qh, &lds_tbl, kTile);
+        total = lds_tbl.tile0[lds_tbl.n];
     }
-    __syncthreads();
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const float2* massml = reinterpret_cast<const float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * p.rows_wg;
-    float* masspart = reinterpret_cast<float*>(ws + p.off_masspart) + (int64_t)unit * p.slots;
-    for (int k = wave; k < p.slots; k += 4) {
-        float c = 0.f;
-        for (int row = lane; row < rows; row += kWave) {
-            const float2 v = massml[(int64_t)k * p.rows_wg + row];
-            c += v.y * __builtin_amdgcn_exp2f(v.x - stat[row].x) * stat[row].y;
+    char* const ws = static_cast<char*>(a.workspace);
+    WavePlace w;
+    w.li = li; w.lg = lg; w.hkv = hkv; w.rows_wg = p.rows_wg; w.ss = split * kSoloWaves + wave;
+    w.t_begin = run_begin(total, p.nsplit * kSoloWaves, w.ss);
+    w.t_end = run_begin(total, p.nsplit * kSoloWaves, w.ss + 1);
+    w.q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
+    w.my_freq = freq.rev[lane];
+    w.cs = cs_lds[wave];
+    w.v_lds = lds + wave * kVTile;
+    w.massml = a.mass ? reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * p.rows_wg : nullptr;
+    auto with_table = [&](auto f) __attribute__((always_inline)) {
+        if constexpr (REG_TABLE) f(rtbl);
+        else f(lds_tbl);
+    };
+
+    RunWalk<false> walk(w.t_begin, w.t_end);
+    auto fetch = [&](Tile& d, TileRegs& r) __attribute__((always_inline)) {
+        with_table([&](const auto& t) { d = walk.next(t, lane); });
+        load_tile(a, s, d, walk.c_tok, hkv, li, lg, r);
+    };
+    Tile d0, d1;
+    TileRegs r0, r1;
+    fetch(d0, r0);
+    fetch(d1, r1);
+    const QueryPart q = query_part(a, w, st, 0);
+    const int q_scale = row_scale<DT>(q);
+    const float down = scale_down(q_scale), mul = a.scale_log2e * scale_of((uint32_t)q_scale);
+    unsigned char* const v_write = w.v_lds + li * kVRow + 64 * lg;
+    const unsigned char* const v_read = w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
+    Parts qt;
+    int q_delta = 0;
+    bool have_parts = false, passed_over = false;
+    auto step = [&](Tile& d, TileRegs& r) __attribute__((always_inline)) {
+        const Tile cd = d;
+        // a tile that is passed over counts as one without tokens (no branch around the body: the compiler would keep the accumulators twice)
+        const bool take = tile_fits(r, cd.ntok, li);
+        const int ntok = take ? cd.ntok : 0;
+        passed_over = passed_over || !take;
+        st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
+        if (!have_parts || cd.delta != q_delta) {
+            have_parts = true;
+            q_delta = cd.delta;
+            put_angles(w.cs, lane, cd.delta, w.my_freq, 1.f);
+            qt = to_parts<DT, PAIRING>(q, down, w.cs, lg);
         }
-        c = wave_sum(c);
-        if (lane == 0) masspart[k] = c;
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *reinterpret_cast<uint4*>(v_write + 16 * tb * kVRow + 16 * c) = unpack8<CF_F16>(r.v[tb][c], take ? scale_of(r.vs[tb]) : 0.f);
+        wave_lds_order();
+        f32x4 sc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) sc[0][tb] = mma_fp4(r.k[tb], (int)r.ks[tb], qt.lo, kLoScale, sc[0][tb]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) sc[0][tb] = Mma<CF_F16>::run(unpack8<CF_F16>(r.k[tb][c], take ? scale_of(r.ks[tb]) : 0.f), qt.hi[c], sc[0][tb]);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(d, r);                                 // the registers are free again
+        __builtin_amdgcn_sched_barrier(0);
+        if (ntok < kTile) {
+            const int lim = ntok - 4 * lg;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sc[0][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[0][e >> 2][e & 3] : -INFINITY;
+        }
+        float pv[1][8];
+        st.softmax(sc, [&](int) { return mul; }, pv);
+        st.template weigh<CF_F16, false>(v_read, pv);
+        wave_lds_order();                            // the next step writes over what others read above
+    };
+    // (left from the middle: with a step skipped the wait for one register set would have to cover the other as well)
+    while (d0.ntok > 0) {
+        step(d0, r0);
+        if (d1.ntok <= 0) break;
+        step(d1, r1);
+    }
+    const bool own = walk.others;
+    if (passed_over) with_table([&](const auto& t) __attribute__((always_inline)) { odd_tiles<DT, PAIRING, 1>(a, s, t, w, st); });
+    if (own) with_table([&](const auto& t) __attribute__((always_inline)) { own_tiles<DT, PAIRING, 1>(a, t, w, st); });
+    st.emit(w.massml, w.rows_wg, w.ss, false, li, lg);
+
+    // ---- the wavefronts' results: wavefront w merges channel block w
+    st.close();
+    if (lg == 0) red_ml[wave][li] = make_float2(st.m_run[0], st.l_run[0]);
+    f32x4* const red = reinterpret_cast<f32x4*>(lds);
+    __syncthreads();                                 // every wavefront is done with its V tile
+#pragma unroll
+    for (int db = 0; db < 8; ++db) red[(wave * 8 + db) * kWave + lane] = st.acc[0][db];
+    __syncthreads();
+    float m = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < kSoloWaves; ++x) m = fmaxf(m, red_ml[x][li].x);
+    const float ms = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < kSoloWaves; ++x) {
+        const float2 v = red_ml[x][li];
+        const float f = __builtin_amdgcn_exp2f(v.x - ms);
+        l += v.y * f;
+        o += red[(x * 8 + wave) * kWave + lane] * f;
+    }
+    o *= l > 0.f ? 1.f / l : l;                      // (a sum that is not a number stays one)
+    const int64_t part = (int64_t)unit * p.nsplit + split;
+    if (wave == 0 && lg == 0) reinterpret_cast<float2*>(ws + p.off_ml)[part * p.rows_wg + li] = make_float2(m, st.trow[0] >= 0 ? l : 0.f);
+    if (p.direct_out) {
+        if (st.trow[0] >= 0) store_out<DT>(a, w.q_first, st.qrow[0], wave, lg, o);
+    } else {
+        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(ws + p.off_opart) + (part * p.rows_wg + li) * kD + 16 * wave + 4 * lg) = o;
     }
 }
 
-// Per-segment attention mass of one query, then S += mass (Alg. 2): sums over units, then over the runs that hold the segment's tiles, in
-// a fixed order; a document slot's first entry adds up all of the slot's entries.
-__global__ __launch_bounds__(256) void q4_mass_kernel(AttnArgs a, Plan p) {
+// ---------------------------------------------------------------------------------------------
+// More row blocks: four wavefronts with NRB blocks each share 32-token tiles.  Bound by the instructions that a SIMD can issue.  Every thread
+// loads 8 bytes of a tile's key codes and of its value codes, three tiles ahead of their use; the key codes go to LDS as they are (a
+// wavefront unpacks them to its matrix operands), the values unpacked, each once per workgroup.  One barrier per tile.
+template <int DT, int PAIRING, int NRB>
+__global__ __launch_bounds__(kRowsThreads, NRB == 1 ? 3 : 2) void attn_q4_rows_kernel(AttnArgs a, RopeFreq freq, Plan p, Scales s) {
+    constexpr int kKBuf = kTile * kRowBytes;
     __shared__ SegTable tbl;
-    __shared__ float col[kMaxEntries + kMaxSplit * kWaves], seg_mass[kMaxEntries];
-    const int b = blockIdx.x, tid = threadIdx.x;
+    // two tiles' key codes, two of values, the workgroup's queries; after the last tile a V tile per wavefront
+    constexpr int kTiles = 2 * (kKBuf + kVTile), kQueries = kRowsWaves * NRB * 16 * kQRow;
+    constexpr int kRowsBytes = kTiles + kQueries > kRowsWaves * kVTile ? kTiles + kQueries : kRowsWaves * kVTile;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[kRowsBytes];
+    __shared__ __attribute__((aligned(16))) float2 cs_lds[kRowsWaves][64];
+    __shared__ uint32_t ks_lds[2][kTile];            // the keys' scale bytes, four of a token
+    __shared__ int odd_lds[2];                       // number of the last tile in a buffer whose scales do not fit fp16
+    __shared__ uint32_t top_lds;
+
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int li = lane & 15, lg = lane >> 4;
+    // grid (split, kv head * row groups + row group, query)
+    const int split = blockIdx.x, b = blockIdx.z;
+    const int hkv = p.n_rg == 1 ? (int)blockIdx.y : (int)div_exact(blockIdx.y, (unsigned)p.n_rg), rg = (int)blockIdx.y - hkv * p.n_rg;
+    const int unit = b * p.units_per_b + (int)blockIdx.y;
     const QueryHead qh = load_query_head(a, b, tid);
-    build_table(a, qh, &tbl, kTile);
-    const float* part = reinterpret_cast<const float*>(static_cast<const char*>(a.workspace) + p.off_masspart) + (int64_t)b * p.units_per_b * p.slots;
-    for (int k = tid; k < p.slots; k += 256) {
-        float c = 0.f;
-        for (int u = 0; u < p.units_per_b; ++u) c += part[(int64_t)u * p.slots + k];
-        col[k] = c;
+    const int tq = max(min(qh.tq_raw, a.max_tq), 0);
+    const int row0 = rg * p.rows_wg;
+    const bool wg_rows = row0 < p.group * tq;        // workgroup-uniform
+    Rows<NRB> st;
+    st.begin(row0 + wave * NRB * 16, p.group * tq, p.group, a.n_q_heads, hkv, li);
+    char* const ws = static_cast<char*>(a.workspace);
+    WavePlace w;
+    w.li = li; w.lg = lg; w.hkv = hkv; w.rows_wg = p.rows_wg; w.ss = split;
+    w.q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
+    w.my_freq = freq.rev[lane];
+    w.cs = cs_lds[wave];
+    w.v_lds = lds + wave * kVTile;
+    w.massml = a.mass ? reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * p.rows_wg + wave * NRB * 16 : nullptr;
+    // the power of two that the workgroup's queries are scaled down by
+    if (tid == 0) { top_lds = 0; odd_lds[0] = odd_lds[1] = -1; }
+    uint32_t top = 0;
+    unsigned char* const q_lds = lds + kTiles + (wave * NRB * 16 + li) * kQRow + 32 * lg;     // (a wavefront reads its own rows only)
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+        const QueryPart q = query_part(a, w, st, rb);
+        top = max(top, largest<DT>(q));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = q.w[i];
     }
-    __syncthreads();
-    const int total = tbl.tile0[tbl.n], nsub = p.nsplit * p.runs;
-    if (tid < tbl.n) {
-        const int ts = tbl.tile0[tid], te = tbl.tile0[tid + 1];
-        float m = 0.f;
-        if (te > ts) {
-            for (int sub = (int)((((int64_t)ts + 1) * nsub - 1) / total); sub < nsub; ++sub) {
-                const int r0 = run_begin(total, nsub, sub), r1 = run_begin(total, nsub, sub + 1);
-                if (r0 >= te) break;
-                if (r1 > r0 && r1 > ts) m += col[tid + sub];
+    build_table(a, qh, &tbl, kTile);                 // (its barriers are after the line above)
+    atomicMax(&top_lds, top);
+    const int total = wg_rows ? tbl.tile0[tbl.n] : 0;
+    w.t_begin = run_begin(total, p.nsplit, split);
+    w.t_end = run_begin(total, p.nsplit, split + 1);
+
+    RunWalk<false> walk(w.t_begin, w.t_end);
+    const int row_bytes = (int)(a.store_ts >> 1), scale_bytes = (int)(a.store_ts >> 5);
+    const int st_tok = tid >> 3, st_part = tid & 7;  // token and 16 channels that the thread stages
+    struct Regs { uint2 k, v; uint32_t vs, ks; };
+    auto fetch = [&](Tile& d, Regs& r) __attribute__((always_inline)) {
+        d = walk.next(tbl, lane);
+        const bool any = d.ntok > 0;
+        const int64_t at = any ? (walk.c_tok + d.tok0) * a.store_ts + (int64_t)hkv * a.store_hs : 0;
+        const int codes = any ? (d.ntok - 1) * row_bytes + kRowBytes : 0, scales = any ? (d.ntok - 1) * scale_bytes + 4 : 0;
+        const int off = st_tok * row_bytes + 8 * st_part;
+        r.k = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(buffer(a.k_store, at >> 1, codes), off, 0, 0));
+        r.v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(buffer(a.v_store, at >> 1, codes), off, 0, 0));
+        r.vs = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(s.v, at >> 5, scales), st_tok * scale_bytes + (st_part >> 1), 0, 0);
+        r.ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(s.k, at >> 5, scales), (lane & 31) * scale_bytes, 0, 0);
+    };
+    auto stage = [&](const Tile& d, const Regs& r, int buf, int number) __attribute__((always_inline)) {
+        unsigned char* const k_buf = lds + buf * kKBuf;
+        unsigned char* const v_buf = lds + 2 * kKBuf + buf * kVTile;
+        *reinterpret_cast<uint2*>(k_buf + 8 * tid) = r.k;
+        const bool fits = fits_f16(r.vs);
+        const float sv = fits ? scale_of(r.vs) : 0.f;
+        unsigned char* const to = v_buf + st_tok * kVRow + 32 * st_part;
+        *reinterpret_cast<uint4*>(to) = unpack8<CF_F16>(r.v.x, sv);
+        *reinterpret_cast<uint4*>(to + 16) = unpack8<CF_F16>(r.v.y, sv);
+        if (tid < kTile) ks_lds[buf][tid] = r.ks;
+        const bool k_fits = fits_f16(r.ks & 255) && fits_f16(r.ks >> 8 & 255) && fits_f16(r.ks >> 16 & 255) && fits_f16(r.ks >> 24);
+        if ((!fits && st_tok < d.ntok) || (!k_fits && tid < d.ntok)) odd_lds[buf] = number;
+    };
+
+    Tile dc, dn;
+    Regs r;
+    fetch(dc, r);
+    __syncthreads();                                 // top_lds
+    const int q_scale = scale_byte_of<DT>(top_lds);
+    const float down = scale_down(q_scale), mul = a.scale_log2e * scale_of((uint32_t)q_scale);
+    // two tables of angles, of the current and of the next segment's tiles, times `down`
+    int cs_slot = 0;
+    auto angles = [&](int slot, int delta) __attribute__((always_inline)) {
+        if (wave == 0) {
+            const float2 c = rope_cos_sin_fast(delta, w.my_freq);
+            cs_lds[slot][lane] = make_float2(c.x * down, c.y * down);
+        }
+    };
+    angles(0, dc.delta);
+    stage(dc, r, 0, 0);
+    fetch(dn, r);
+    Parts qt[NRB];
+    int q_delta = 0, number = 0;
+    bool have_parts = false, passed_over = false;
+    const unsigned char* const v_read = lds + 2 * kKBuf + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
+    // Step: tile `dc` is in buffer `buf`; the one after it, dn, is on its way to registers since a step ago, from where it goes to the other
+    // buffer, and the next one is requested.  (Two sets of registers, two tiles ahead: the compiler waits for both at the loop's head.)
+    for (int buf = 0; dc.ntok > 0; buf ^= 1, ++number) {
+        __syncthreads();                             // tile `dc` is staged; every wavefront is done with the other buffer
+        const Tile cd = dc;
+        const bool turn_next = dn.ntok > 0 && dn.delta != cd.delta;
+        const int next_delta = dn.delta;
+        dc = dn;
+        stage(dn, r, buf ^ 1, number + 1);
+        fetch(dn, r);
+        const bool take = odd_lds[buf] != number;
+        i32x4 kc[2];
+        uint32_t ks[2];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+            kc[tb] = *reinterpret_cast<const i32x4*>(lds + buf * kKBuf + (16 * tb + li) * kRowBytes + 16 * lg);
+            ks[tb] = reinterpret_cast<const uint8_t*>(ks_lds[buf])[4 * (16 * tb + li) + lg];
+        }
+        st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
+        if (!have_parts || cd.delta != q_delta) {
+            have_parts = true;
+            q_delta = cd.delta;
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) {
+                QueryPart q;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q.w[i] = *reinterpret_cast<const uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1));
+                qt[rb] = to_parts<DT, PAIRING>(q, 1.f, cs_lds[cs_slot], lg);
             }
         }
-        a.mass[(int64_t)b * a.seg_stride + tid] = m;
-        seg_mass[tid] = m;
+        if (turn_next) {
+            cs_slot ^= 1;
+            angles(cs_slot, next_delta);
+        }
+        const int ntok = take ? cd.ntok : 0;
+        passed_over = passed_over || !take;
+        f32x4 sc[NRB][2];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) sc[rb][tb] = mma_fp4(kc[tb], (int)ks[tb], qt[rb].lo, kLoScale, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                const uint4 kf = unpack8<CF_F16>(kc[tb][c], scale_of(ks[tb]));
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb) sc[rb][tb] = Mma<CF_F16>::run(kf, qt[rb].hi[c], sc[rb][tb]);
+            }
+        if (ntok < kTile) {
+            const int lim = ntok - 4 * lg;
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
+        }
+        float pv[NRB][8];
+        st.softmax(sc, [&](int) { return mul; }, pv);
+        st.template weigh<CF_F16, false>(v_read + buf * kVTile, pv);
     }
-    __syncthreads();
-    if (a.score_accum == nullptr || tid >= tbl.n) return;
-    const int d = tbl.doc[tid];
+    const bool own = walk.others;
+    __syncthreads();                                 // the buffers become the wavefronts' own
+    if (passed_over) odd_tiles<DT, PAIRING, NRB>(a, s, tbl, w, st);
+    if (own) own_tiles<DT, PAIRING, NRB>(a, tbl, w, st);
+    st.emit(w.massml, w.rows_wg, w.ss, false, li, lg);
+    st.close();
+    const int64_t part = (int64_t)unit * p.nsplit + split;
+    float2* const ml = reinterpret_cast<float2*>(ws + p.off_ml) + part * p.rows_wg + wave * NRB * 16;
+    float* const opart = reinterpret_cast<float*>(ws + p.off_opart) + (part * p.rows_wg + wave * NRB * 16) * kD;
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+        const float l = st.l_run[rb], inv = l > 0.f ? 1.f / l : l;       // (a sum that is not a number stays one)
+        if (lg == 0) ml[16 * rb + li] = make_float2(st.m_run[rb], st.trow[rb] >= 0 ? l : 0.f);
+        if (st.trow[rb] < 0) continue;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+            if (p.direct_out) store_out<DT>(a, w.q_first, st.qrow[rb], db, lg, st.acc[rb][db] * inv);
+            else *reinterpret_cast<f32x4*>(opart + (16 * rb + li) * kD + 16 * db + 4 * lg) = st.acc[rb][db] * inv;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Merges the splits' partial rows, a wavefront per row: lane s holds the statistics of split s, then a lane two channels.  A row's own
+// (maximum, sum) replaces split 0's, for the mass kernel.
+template <int DT>
+__global__ __launch_bounds__(256) void q4_combine_kernel(AttnArgs a, Plan p) {
+    const int b = blockIdx.z, unit = b * p.units_per_b + (int)blockIdx.y;
+    const int hkv = p.n_rg == 1 ? (int)blockIdx.y : (int)div_exact(blockIdx.y, (unsigned)p.n_rg), rg = (int)blockIdx.y - hkv * p.n_rg;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int row = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)threadIdx.x / kWave);
+    char* ws = static_cast<char*>(a.workspace);
+    const int64_t first = (int64_t)unit * p.nsplit * p.rows_wg + row;
+    float2* const ml = reinterpret_cast<float2*>(ws + p.off_ml) + first;
+    const float2* const opart = reinterpret_cast<const float2*>(ws + p.off_opart) + first * (kD / 2) + lane;
+    const int q0 = a.q_off[b], q1 = a.q_off[b + 1];
+    constexpr int kBatch = 8;
+    // everything is requested before anything is waited for; loads past the splits read the last one again
+    const float2 stat = ml[(int64_t)min(lane, p.nsplit - 1) * p.rows_wg];
+    float2 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) v[i] = opart[(int64_t)min(i, p.nsplit - 1) * p.rows_wg * (kD / 2)];
+    const int tq = max(min(q1 - q0, a.max_tq), 0);
+    const int m2 = rg * p.rows_wg + row;
+    if (m2 >= p.group * tq) return;
+    const float mx = wave_max(lane < p.nsplit ? stat.x : -INFINITY);
+    const float m = mx == -INFINITY ? 0.f : mx;
+    const float weight = lane < p.nsplit ? stat.y * __builtin_amdgcn_exp2f(stat.x - m) : 0.f;
+    const float l = wave_sum(weight);
+    float2 o = make_float2(0.f, 0.f);
+    for (int s0 = 0; s0 < p.nsplit; s0 += kBatch) {
+        float2 x[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) x[i] = v[i];
+        if (s0 + kBatch < p.nsplit) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) v[i] = opart[(int64_t)min(s0 + kBatch + i, p.nsplit - 1) * p.rows_wg * (kD / 2)];
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (s0 + i >= p.nsplit) break;
+            const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), s0 + i));
+            o.x += x[i].x * f;
+            o.y += x[i].y * f;
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : l;
+    const int t = (int)div_exact((unsigned)m2, (unsigned)p.group), g = m2 - t * p.group;
+    uint32_t* op = static_cast<uint32_t*>(a.out) + (((int64_t)q0 + t) * a.n_q_heads + hkv * p.group + g) * (kD / 2) + lane;
+    *op = Mma<DT>::pack(o.x * inv, o.y * inv);
+    if (a.mass && lane == 0) ml[0] = make_float2(mx, l);
+}
+
+// Per-segment attention mass, a workgroup per table entry: over the units, the runs that hold the segment's tiles and the rows, sum * exp2(reference -
+// row maximum) / row sum, in a fixed order.  Then S += mass (Alg. 2): a document slot's first entry works out the masses of all of the slot's
+// entries and adds them up in table order.
+__global__ __launch_bounds__(256) void q4_mass_kernel(AttnArgs a, Plan p) {
+    __shared__ SegTable tbl;
+    __shared__ float part_sum[4];
+    const int b = blockIdx.y, entry = blockIdx.x, tid = threadIdx.x;
+    const QueryHead qh = load_query_head(a, b, tid);
+    build_table(a, qh, &tbl, kTile);
+    if (entry >= tbl.n) return;
+    const char* ws = static_cast<const char*>(a.workspace);
+    const int tq = max(min(qh.tq_raw, a.max_tq), 0), n_rows = p.group * tq;
+    const int total = tbl.tile0[tbl.n], nsub = p.nsplit * p.runs;
+    auto mass_of = [&](int s) {
+        const int ts = tbl.tile0[s], te = tbl.tile0[s + 1];
+        float sum = 0.f;
+        if (te > ts) {
+            const int sub0 = run_of(total, nsub, ts), sub1 = run_of(total, nsub, te - 1);
+            const int n_sub = sub1 - sub0 + 1;
+            // items: unit, run, row; threads take rows of one (unit, run) side by side
+            const int rows = min(p.rows_wg, 256), per = 256 / rows;      // rows_wg is a power of two
+            const int row = tid & (rows - 1), first = tid / rows;
+            for (int i = first; i < p.units_per_b * n_sub; i += per) {
+                const int u = (int)div_exact((unsigned)i, (unsigned)n_sub), sub = sub0 + i - u * n_sub;
+                // a run between a segment's first and last may own no tile at all: its slot was not written
+                if (run_begin(total, nsub, sub) >= run_begin(total, nsub, sub + 1)) continue;
+                const int rg = u - (int)div_exact((unsigned)u, (unsigned)p.n_rg) * p.n_rg;
+                const int64_t unit = (int64_t)b * p.units_per_b + u;
+                if (rg * p.rows_wg + row >= n_rows) continue;
+                const float2 v = reinterpret_cast<const float2*>(ws + p.off_massml)[(unit * p.slots + s + sub) * p.rows_wg + row];
+                const float2 r = reinterpret_cast<const float2*>(ws + p.off_ml)[unit * p.nsplit * p.rows_wg + row];
+                const float m = r.x == -INFINITY ? 0.f : r.x;
+                sum += v.y * __builtin_amdgcn_exp2f(v.x - m) * (r.y > 0.f ? 1.f / r.y : r.y);
+            }
+        }
+        sum = wave_sum(sum);
+        __syncthreads();
+        if ((tid & (kWave - 1)) == 0) part_sum[tid / kWave] = sum;
+        __syncthreads();
+        return ((part_sum[0] + part_sum[1]) + part_sum[2]) + part_sum[3];
+    };
+    const float mine = mass_of(entry);
+    if (tid == 0) a.mass[(int64_t)b * a.seg_stride + entry] = mine;
+    if (a.score_accum == nullptr) return;
+    const int d = tbl.doc[entry];
     if (d < 0 || d >= a.score_stride) return;
-    float sum = seg_mass[tid];
-    for (int j = 0; j < tbl.n; ++j) {
+    float sum = mine;
+    for (int j = 0; j < tbl.n; ++j) {                // workgroup-uniform
         if (tbl.doc[j] != d) continue;
-        if (j < tid) return;
-        if (j > tid) sum += seg_mass[j];
+        if (j < entry) return;
+        if (j > entry) sum += mass_of(j);
     }
-    a.score_accum[(int64_t)b * a.score_stride + d] += sum;
+    if (tid == 0) a.score_accum[(int64_t)b * a.score_stride + d] += sum;
 }
 
 }  // namespace
@@ -813,39 +1059,34 @@ cf_status launch_attention_q4(const AttnArgs& a, const q4::Scales& sc, const Rop
         set_error("neither batch nor n_kv_heads * row groups may exceed 65535 on this path");
         return CF_ERR_UNSUPPORTED;
     }
-    const dim3 grid((unsigned)p.nsplit, (unsigned)p.units_per_b, (unsigned)a.batch), block(kThreads);
-    auto go = [&](auto dt, auto pairing, auto nrb) {
-        constexpr int DT = decltype(dt)::value, PAIRING = decltype(pairing)::value, NRB = decltype(nrb)::value;
-        // (with two row blocks a wavefront has no registers left for a table)
-        if constexpr (NRB == 1) {
-            if (a.seg_stride <= kWave) {
-                hipLaunchKernelGGL((attn_q4_kernel<DT, PAIRING, 1, true>), grid, block, 0, s, a, f, p, sc);
-                return;
-            }
+    const dim3 grid((unsigned)p.nsplit, (unsigned)p.units_per_b, (unsigned)a.batch);
+    auto go = [&](auto dt, auto pairing) {
+        constexpr int DT = decltype(dt)::value, PAIRING = decltype(pairing)::value;
+        if (p.solo) {
+            if (a.seg_stride <= kWave) hipLaunchKernelGGL((attn_q4_solo_kernel<DT, PAIRING, true>), grid, dim3(kSoloThreads), 0, s, a, f, p, sc);
+            else hipLaunchKernelGGL((attn_q4_solo_kernel<DT, PAIRING, false>), grid, dim3(kSoloThreads), 0, s, a, f, p, sc);
+        } else if (p.nrb == 1) {
+            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 1>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
+        } else {
+            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 2>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
         }
-        hipLaunchKernelGGL((attn_q4_kernel<DT, PAIRING, NRB, false>), grid, block, 0, s, a, f, p, sc);
-    };
-    auto by_rows = [&](auto dt, auto pairing) {
-        if (p.nrb == 1) go(dt, pairing, std::integral_constant<int, 1>{});
-        else go(dt, pairing, std::integral_constant<int, 2>{});
     };
     auto by_pairing = [&](auto dt) {
-        if (a.pairing == CF_ROPE_HALF) by_rows(dt, std::integral_constant<int, CF_ROPE_HALF>{});
-        else by_rows(dt, std::integral_constant<int, CF_ROPE_INTERLEAVED>{});
+        if (a.pairing == CF_ROPE_HALF) go(dt, std::integral_constant<int, CF_ROPE_HALF>{});
+        else go(dt, std::integral_constant<int, CF_ROPE_INTERLEAVED>{});
     };
     const bool bf16 = a.dtype == CF_BF16;
     if (bf16) by_pairing(std::integral_constant<int, CF_BF16>{});
     else by_pairing(std::integral_constant<int, CF_F16>{});
     CF_HIP(hipGetLastError());
     if (!p.direct_out) {
-        const dim3 rows((unsigned)(p.rows_wg + 7) / 8, (unsigned)p.units_per_b, (unsigned)a.batch);
+        const dim3 rows((unsigned)p.rows_wg / 4, (unsigned)p.units_per_b, (unsigned)a.batch);
         if (bf16) hipLaunchKernelGGL(q4_combine_kernel<CF_BF16>, rows, dim3(256), 0, s, a, p);
         else hipLaunchKernelGGL(q4_combine_kernel<CF_F16>, rows, dim3(256), 0, s, a, p);
         CF_HIP(hipGetLastError());
     }
     if (a.mass != nullptr) {
-        hipLaunchKernelGGL(q4_slots_kernel, dim3((unsigned)p.units), dim3(256), 0, s, a, p);
-        hipLaunchKernelGGL(q4_mass_kernel, dim3((unsigned)a.batch), dim3(256), 0, s, a, p);
+        hipLaunchKernelGGL(q4_mass_kernel, dim3((unsigned)a.seg_stride, (unsigned)a.batch), dim3(256), 0, s, a, p);
         CF_HIP(hipGetLastError());
     }
     return CF_OK;

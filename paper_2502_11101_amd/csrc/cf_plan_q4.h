@@ -12,7 +12,8 @@
 namespace cf {
 namespace q4 {
 
-constexpr int kWaves = 8;           // wavefronts of a workgroup
+constexpr int kSoloWaves = 8;       // wavefronts of attn_q4_solo_kernel's workgroups, each with tiles of its own
+constexpr int kRowsWaves = 4;       // of attn_q4_rows_kernel's, each with rows of its own
 constexpr int kD = 128;
 constexpr int kTile = 32;           // tokens per tile
 constexpr int kMaxSplit = 64;
@@ -20,14 +21,14 @@ constexpr int kMaxEntries = 256;    // table entries of a query
 
 struct Plan {
     int group;          // query heads per kv head
+    int solo;           // attn_q4_solo_kernel (one 16-row block), else attn_q4_rows_kernel
     int nrb;            // 16-row blocks of a wavefront
-    int row_waves;      // wavefronts of a workgroup that own different rows; the others of its kWaves stream other tiles
-    int runs;           // runs of tiles per workgroup: kWaves / row_waves
-    int rows_wg;        // rows a workgroup has room for: 16 * nrb * row_waves
+    int runs;           // runs of tiles per workgroup
+    int rows_wg;        // rows a workgroup has room for
     int n_rg;           // row groups (workgroups side by side) per (query, kv head)
     int units_per_b, units, nsplit, slots;
     int direct_out;     // one split: the attention kernel writes the output rows itself
-    size_t off_ml, off_opart, off_massml, off_masspart, total;
+    size_t off_ml, off_opart, off_massml, total;
 };
 
 inline int64_t plan_tiles(int seg_stride, int64_t max_kv_tokens) { return max_kv_tokens / kTile + seg_stride; }
@@ -36,16 +37,16 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     Plan p;
     p.group = n_q_heads / n_kv_heads;
     const int64_t blocks = ((int64_t)p.group * max_tq + 15) / 16;
-    p.nrb = blocks > 1 ? 2 : 1;
-    const int64_t waves = (blocks + p.nrb - 1) / p.nrb;
-    p.row_waves = waves > 4 ? 8 : waves > 2 ? 4 : waves > 1 ? 2 : 1;
-    p.runs = kWaves / p.row_waves;
-    p.rows_wg = 16 * p.nrb * p.row_waves;
-    p.n_rg = (int)((waves + p.row_waves - 1) / p.row_waves);
+    p.solo = blocks <= 1;
+    p.nrb = blocks > 4 ? 2 : 1;
+    p.runs = p.solo ? kSoloWaves : 1;
+    p.rows_wg = p.solo ? 16 : 16 * p.nrb * kRowsWaves;
+    p.n_rg = (int)std::max<int64_t>((16 * blocks + p.rows_wg - 1) / p.rows_wg, 1);
     p.units_per_b = n_kv_heads * p.n_rg;
     p.units = batch * p.units_per_b;
     const int64_t tiles = plan_tiles(seg_stride, max_kv_tokens);
-    p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({256 / std::max(p.units, 1), tiles / (2 * p.runs), (int64_t)kMaxSplit}), 1);
+    const int64_t room = p.solo ? 256 : 512, least = p.solo ? 2 * p.runs : 4;
+    p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({room / std::max(p.units, 1), tiles / least, (int64_t)kMaxSplit}), 1);
     p.direct_out = p.nsplit == 1;
     p.slots = seg_stride + p.nsplit * p.runs;
     size_t off = 0;
@@ -54,7 +55,6 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.off_ml = take(rows * 2 * sizeof(float));
     p.off_opart = take(p.direct_out ? 0 : rows * kD * sizeof(float));
     p.off_massml = take((size_t)p.units * p.slots * p.rows_wg * 2 * sizeof(float));
-    p.off_masspart = take((size_t)p.units * p.slots * sizeof(float));
     p.total = off;
     return p;
 }
