@@ -2,18 +2,18 @@
 //
 // A stored key or value row is 128 codes of four bits and four scale bytes (32 channels each).  What is moved to other positions is the query
 // and not the keys: (R_delta k) . q = k . (R_-delta q), once per segment instead of once per key (Eq. 5), and the keys stay exact.
-// Scores.  The turned query, scaled by a power of two of its row, enters as two parts: its fp16 value, multiplied with the keys unpacked to fp16
-// (exact: at most two significant bits and an exponent inside fp16's) by v_mfma_f32_16x16x32_f16, and the remainder in e4m3, multiplied with
-// the codes and scale bytes as they lie in memory by v_mfma_scale_f32_16x16x128_f8f6f4: 15 bits of the query in all.  (That instruction alone, with
-// three e4m3 terms, costs the same matrix cycles and no unpacking, but sums its 128 products with an error of up to 2^-13 of the
-// largest one: attention masses were off by 2e-6 to 5e-6, by ... with the main part in fp16.)
+// Scores.  The turned query, scaled by a power of two, is split into two fp16 terms (22 bits); the keys, unpacked to fp16, are exact (at most two
+// significant bits and an exponent inside fp16's), so that scores are right to fp32's accuracy on v_mfma_f32_16x16x32_f16.  (The scaled
+// 4-bit instruction, v_mfma_scale_f32_16x16x128_f8f6f4, takes the codes as they lie in memory against a query of e4m3 terms at the same matrix
+// cycles, but sums its 128 products with an error of up to 2^-13 of the largest one: attention masses were off by 2e-6 to 5e-6, and with an fp16 term
+// and one e4m3 term on that instruction by 7e-7 to 1.1e-6.)
 // Values are unpacked to fp16, staged in LDS and read transposed; probabilities are rounded to fp16 (2^-11), sums, maxima and accumulators
-// are fp32.  Tiles with a scale outside fp16's exponents are left to a second pass over the run in which keys meet a query of three e4m3 terms
-// and values and probabilities are bf16, the latter as value and remainder.
+// are fp32.  Tiles with a scale outside fp16's exponents are left to a second pass over the run, in bf16: queries of three terms,
+// probabilities as value and remainder.
 //
 // Work: the rows that share a kv head (row m = t * group + head) are cut into 16-row blocks.
 //   * One block (decode steps): attn_q4_solo_kernel, each of eight wavefronts streams a run of 32-token tiles of its own; they meet in LDS at the end.
-//   * More: attn_q4_rows_kernel, four wavefronts own one or two blocks each and share the tiles that they stage together.
+//   * More: attn_q4_rows_kernel, eight wavefronts that share the tiles that they stage together.
 // Splits (workgroups of the same rows) leave fp32 partial rows that q4_combine_kernel merges; q4_mass_kernel reduces the (reference, sum) pairs
 // that the wavefronts leave per row and segment where masses are wanted.
 #include "cf_attn_tile.h"
@@ -38,14 +38,11 @@ using attn::wave_lds_order;
 namespace {
 
 constexpr int kSoloThreads = kSoloWaves * kWave, kRowsThreads = kRowsWaves * kWave;
-constexpr int kVRow = 288;                           // bytes per token of a staged V tile
-constexpr int kVTile = kTile * kVRow;
+constexpr int kKRow = 272, kVRow = 288;              // bytes per token of a staged tile
+constexpr int kKTile = kTile * kKRow, kVTile = kTile * kVRow;
 constexpr int kRowBytes = 64;                        // codes of a row
 constexpr int kQRow = 272;                           // bytes per row of queries in LDS
 constexpr float kProbLimit = attn::kProbLimit;
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // run i of a list of `total` tiles owns [total*i/n, total*(i+1)/n) (n at most 512, so that shorter lists need no 64-bit division)
 __device__ __forceinline__ int run_begin(int total, int n, int i) {
@@ -58,44 +55,90 @@ __device__ __forceinline__ int run_of(int total, int n, int x) {
     return (int)((((int64_t)x + 1) * n - 1) / total);
 }
 
+// The first segment of a kind (of the own block, or of the store) whose tiles reach past tile x; -1: none.  `prev`: a segment that is not behind it.
+template <bool OWN>
+__device__ __forceinline__ int find_kind(const SegTable& t, int x, int lane, int prev) {
+    for (int s0 = prev < 0 ? 0 : prev & ~(kWave - 1); s0 < t.n; s0 += kWave) {
+        const int idx = s0 + lane;
+        const uint64_t hit = __ballot(idx < t.n && t.tile0[idx + 1] > x && (t.self[idx] != 0) == OWN && t.vis[idx] > 0);
+        if (hit) return s0 + __builtin_ctzll(hit);
+    }
+    return -1;
+}
+template <bool OWN>
+__device__ __forceinline__ int find_kind(const RegSegTable& t, int x, int lane, int) {
+    const uint64_t hit = __ballot(lane < t.n && t.t1 > x && (t.self != 0) == OWN && t.vis > 0);
+    return hit ? __builtin_ctzll(hit) : -1;
+}
+__device__ __forceinline__ int first_tile(const SegTable& t, int s) { return __builtin_amdgcn_readfirstlane(t.tile0[s]); }
+__device__ __forceinline__ int first_tile(const RegSegTable& t, int s) { return __builtin_amdgcn_readlane(t.t0, s); }
+struct SegFields { int first, end, vis, delta; int64_t tok; };
+__device__ __forceinline__ int64_t scalar64(int64_t x) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ SegFields fields(const SegTable& t, int s) {
+    auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    return {scalar(t.tile0[s]), scalar(t.tile0[s + 1]), scalar(t.vis[s]), scalar(t.delta[s]), scalar64(t.tok[s])};
+}
+__device__ __forceinline__ SegFields fields(const RegSegTable& t, int s) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)t.tok, s), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)t.tok >> 32), s);
+    return {__builtin_amdgcn_readlane(t.t0, s), __builtin_amdgcn_readlane(t.t1, s), __builtin_amdgcn_readlane(t.vis, s), __builtin_amdgcn_readlane(t.delta, s),
+            (int64_t)((uint64_t)hi << 32 | lo)};
+}
+// whether a run holds tiles of the kind
+template <bool OWN, class Table>
+__device__ __forceinline__ bool holds(const Table& t, int begin, int end, int lane) {
+    const int s = begin < end ? find_kind<OWN>(t, begin, lane, -1) : -1;
+    return s >= 0 && first_tile(t, s) < end;
+}
+
 // Walks the tiles of a run that lie in the store, or (OWN) in the own block.
 template <bool OWN>
 struct RunWalk {
     int next_tile, t_end;
     int c_seg = -1, c_first = 0, c_end = 0, c_vis = 0, c_delta = 0;
     int64_t c_tok = 0;          // first token of the cached segment in its tensor
-    bool others = false;        // tiles of the other kind were passed over
 
     __device__ __forceinline__ RunWalk(int begin, int end) : next_tile(begin), t_end(end) {}
 
+    // to the next tile of the kind, or to the end
+    template <class Table>
+    __device__ __forceinline__ void settle(const Table& tbl, int lane) {
+        if (next_tile >= t_end || next_tile < c_end) return;
+        const int s = find_kind<OWN>(tbl, next_tile, lane, c_seg);
+        if (s < 0) {
+            next_tile = t_end;
+            return;
+        }
+        const SegFields f = fields(tbl, s);
+        c_seg = s;
+        c_first = f.first;
+        c_end = f.end;
+        c_vis = f.vis;
+        c_delta = f.delta;
+        c_tok = f.tok;
+        next_tile = max(next_tile, c_first);
+    }
     // The next tile, or one with ntok == 0 when none is left.
     template <class Table>
     __device__ __forceinline__ Tile next(const Table& tbl, int lane) {
         Tile d;
         d.seg = 0; d.tok0 = 0; d.ntok = 0; d.delta = 0; d.self = 0;
-        while (next_tile < t_end) {
-            if (next_tile >= c_end) {
-                const attn::FoundSegment f = attn::find_segment(tbl, next_tile, lane, c_seg);
-                c_seg = f.seg;
-                c_first = f.first;
-                c_end = f.end;
-                c_vis = f.vis;
-                c_delta = f.delta;
-                c_tok = f.tok;
-                if ((f.self != 0) != OWN) {
-                    others = true;
-                    next_tile = f.end;
-                    continue;
-                }
-            }
+        settle(tbl, lane);
+        if (next_tile < t_end) {
             d.seg = c_seg;
             d.tok0 = (next_tile - c_first) * kTile;
-            d.ntok = max(0, min(kTile, c_vis - d.tok0));
+            d.ntok = min(kTile, c_vis - d.tok0);
             d.delta = c_delta;
             ++next_tile;
-            break;
         }
         return d;
+    }
+    template <class Table>
+    __device__ __forceinline__ void skip(const Table& tbl, int lane) {
+        settle(tbl, lane);
+        ++next_tile;
     }
 };
 
@@ -185,86 +228,50 @@ __device__ __forceinline__ int row_scale(const QueryPart& q) {
     return scale_byte_of<DT>(top);
 }
 
+// the same for the block as a whole
+template <int DT>
+__device__ __forceinline__ int block_scale(const QueryPart& q) {
+    uint32_t top = largest<DT>(q);
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    return __builtin_amdgcn_readfirstlane(scale_byte_of<DT>(top));
+}
+
 __device__ __forceinline__ float scale_down(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
 
-// A 16-row block of turned queries: fp16 values (hi[s]: channels 32 lg + 8 s .. + 7) and what is left, 2^11 times larger, in e4m3.
-constexpr int kLoScale = 127 - 11;
-struct Parts { uint4 hi[4]; i32x8 lo; };
+// two floats as 16-bit values and what is left of them
+template <int DT>
+__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = Mma<DT>::pack(x, y);
+    lo = Mma<DT>::pack(x - Mma<DT>::lo(hi), y - Mma<DT>::hi(hi));
+}
+template <int DT>
+__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
+    split2<DT>(v[0], v[1], hi.x, lo.x);
+    split2<DT>(v[2], v[3], hi.y, lo.y);
+    split2<DT>(v[4], v[5], hi.z, lo.z);
+    split2<DT>(v[6], v[7], hi.w, lo.w);
+}
 
-// `down`: scales the queries, if `cs` does not.
-template <int DT, int PAIRING>
-__device__ __forceinline__ Parts to_parts(const QueryPart& q, float down, const float2* cs, int lg) {
+// A 16-row block of turned queries as matrix operands of type OT, value and remainder.  A matrix product does not mind the order of its channels as
+// long as both sides have the same: operand c of a lane holds channels 16 lg + 8 c .. + 7 (c < 2) or 64 + 16 lg + 8 (c - 2) .. + 7, which are those
+// that the lane turns.
+struct Parts { uint4 hi[4], lo[4]; };
+template <int DT, int PAIRING, int OT>
+__device__ __forceinline__ Parts to_parts(const QueryPart& q, const float2* cs, int lg) {
     Parts r;
-    uint32_t h[2][8];                                // fp16 pairs of either half
-    auto split = [&](float (&v)[4], int w, uint32_t (&h)[8], int at) __attribute__((always_inline)) {
-        h[at] = Mma<CF_F16>::pack(v[0] * down, v[1] * down);
-        h[at + 1] = Mma<CF_F16>::pack(v[2] * down, v[3] * down);
-        auto rest = [&](int i, float x) { return fmaf(v[i], down, -x) * 2048.f; };       // exact
-        const int packed = __builtin_amdgcn_cvt_pk_fp8_f32(rest(0, Mma<CF_F16>::lo(h[at])), rest(1, Mma<CF_F16>::hi(h[at])), 0, false);
-        r.lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(rest(2, Mma<CF_F16>::lo(h[at + 1])), rest(3, Mma<CF_F16>::hi(h[at + 1])), packed, true);
-    };
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        float a[4], b[4];
-        turn4<DT, PAIRING>(q, n, cs, lg, a, b);
-        split(a, n, h[0], 2 * n);
-        split(b, 4 + n, h[1], 2 * n);
+    for (int c = 0; c < 2; ++c) {
+        float a0[4], b0[4], a1[4], b1[4];
+        turn4<DT, PAIRING>(q, 2 * c, cs, lg, a0, b0);
+        turn4<DT, PAIRING>(q, 2 * c + 1, cs, lg, a1, b1);
+        const float va[8] = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
+        const float vb[8] = {b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
+        split8<OT>(va, r.hi[c], r.lo[c]);
+        split8<OT>(vb, r.hi[2 + c], r.lo[2 + c]);
         __builtin_amdgcn_sched_barrier(0);           // few floats at a time
     }
-    // A lane has turned channels 16 lg .. and 64 + 16 lg .. (both of a slice), the fp16 fragments want 32 lg ...: lane groups 0 | 1 | 2 | 3 take the
-    // first halves of groups 0, 1 | 2, 3 and the second halves of 0, 1 | 2, 3
-    uint32_t f[16];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const auto x = __builtin_amdgcn_permlane32_swap(h[0][i], h[1][i], false, false);
-        const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
-        f[i] = y[0];
-        f[8 + i] = y[1];
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s) r.hi[s] = make_uint4(f[4 * s], f[4 * s + 1], f[4 * s + 2], f[4 * s + 3]);
     return r;
-}
-
-// The same as three terms of e4m3, 16 times larger from one to the next, for keys of any scale.
-constexpr int kTerms = 3;
-struct Terms { i32x8 t[kTerms]; };
-
-template <int DT, int PAIRING>
-__device__ __forceinline__ Terms to_terms(const QueryPart& q, int scale, const float2* cs, int lg) {
-    const float down = scale_down(scale);
-    Terms r;
-    auto split = [&](float (&v)[4], int w) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] *= down;
-#pragma unroll
-        for (int k = 0; k < kTerms; ++k) {
-            int packed = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-            packed = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], packed, true);
-            r.t[k][w] = packed;
-            if (k + 1 < kTerms) {                    // what is left: exact
-                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(packed, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(packed, true);
-                v[0] = (v[0] - lo[0]) * 16.f;
-                v[1] = (v[1] - lo[1]) * 16.f;
-                v[2] = (v[2] - hi[0]) * 16.f;
-                v[3] = (v[3] - hi[1]) * 16.f;
-            }
-        }
-    };
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        float a[4], b[4];
-        turn4<DT, PAIRING>(q, n, cs, lg, a, b);
-        split(a, n);
-        split(b, 4 + n);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    return r;
-}
-
-__device__ __forceinline__ f32x4 mma_fp4(i32x4 k, int k_scale, const i32x8& q, int q_scale, f32x4 c) {
-    const i32x8 a = {k[0], k[1], k[2], k[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, c, 4, 0, 0, k_scale, 0, q_scale);
 }
 
 // eight 16-bit values, zeros where they are not finite; any: whether there were some
@@ -279,20 +286,6 @@ __device__ __forceinline__ uint4 finite8(uint4 v, bool& any) {
         w[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// two floats as 16-bit values and what is left of them
-template <int DT>
-__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
-    hi = Mma<DT>::pack(x, y);
-    lo = Mma<DT>::pack(x - Mma<DT>::lo(hi), y - Mma<DT>::hi(hi));
-}
-template <int DT>
-__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
-    split2<DT>(v[0], v[1], hi.x, lo.x);
-    split2<DT>(v[2], v[3], hi.y, lo.y);
-    split2<DT>(v[4], v[5], hi.z, lo.z);
-    split2<DT>(v[6], v[7], hi.w, lo.w);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -429,8 +422,9 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* base, int64
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base) + off), 0, range, 0x00020000);
 }
 
-// A tile of the store for a wavefront on its own: token 16 tb + li, 32 channels from 32 lg on.
-struct TileRegs { i32x4 k[2], v[2]; uint32_t ks[2], vs[2]; };
+// A tile of the store for a wavefront on its own: of token 16 tb + li the key channels 16 lg .. + 15 and 64 + 16 lg .. + 15 with all four scales,
+// and 32 value channels from 32 lg on.
+struct TileRegs { uint2 k[2][2]; uint4 v[2]; uint32_t ks[2], vs[2]; };
 __device__ __forceinline__ void load_tile(const AttnArgs& a, const Scales& s, const Tile& d, int64_t seg_tok, int hkv, int li, int lg, TileRegs& r) {
     const int row_bytes = (int)(a.store_ts >> 1), scale_bytes = (int)(a.store_ts >> 5);
     // rows past a ragged tile's end, and everything where no tile is left, lie past the range and read as zero
@@ -441,15 +435,32 @@ __device__ __forceinline__ void load_tile(const AttnArgs& a, const Scales& s, co
     const auto sk = buffer(s.k, at >> 5, scales), sv = buffer(s.v, at >> 5, scales);
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-        const int off = (16 * tb + li) * row_bytes + 16 * lg, soff = (16 * tb + li) * scale_bytes + lg;
-        r.k[tb] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
-        r.v[tb] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
-        r.ks[tb] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sk, soff, 0, 0);
-        r.vs[tb] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sv, soff, 0, 0);
+        const int off = (16 * tb + li) * row_bytes, soff = (16 * tb + li) * scale_bytes;
+        r.k[tb][0] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rk, off + 8 * lg, 0, 0));
+        r.k[tb][1] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rk, off + 8 * lg + 32, 0, 0));
+        r.v[tb] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, off + 16 * lg, 0, 0));
+        r.ks[tb] = __builtin_amdgcn_raw_buffer_load_b32(sk, soff, 0, 0);
+        r.vs[tb] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sv, soff + lg, 0, 0);
     }
 }
-__device__ __forceinline__ bool tile_fits(const TileRegs& r, int ntok, int li) {
-    return __all(((fits_f16(r.ks[0]) && fits_f16(r.vs[0])) || li >= ntok) && ((fits_f16(r.ks[1]) && fits_f16(r.vs[1])) || 16 + li >= ntok));
+// operand c of the keys 16 tb .. + 15 (see Parts)
+template <int DT>
+__device__ __forceinline__ uint4 key_operand(const TileRegs& r, int tb, int c, int lg) {
+    const uint2 w = r.k[tb][c >> 1];
+    return unpack8<DT>(c & 1 ? w.y : w.x, scale_of(__builtin_amdgcn_ubfe(r.ks[tb], 16 * (c >> 1) + 8 * (lg >> 1), 8)));
+}
+__device__ __forceinline__ bool tile_fits(const TileRegs& r, int ntok, int li, int lg) {
+    bool fits = true;
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+        fits = fits && ((fits_f16(__builtin_amdgcn_ubfe(r.ks[tb], 8 * lg, 8)) && fits_f16(r.vs[tb])) || 16 * tb + li >= ntok);
+    return __all(fits);
+}
+__device__ __forceinline__ void stage_values(unsigned char* to, uint4 codes, float scale) {
+    reinterpret_cast<uint4*>(to)[0] = unpack8<CF_F16>(codes.x, scale);
+    reinterpret_cast<uint4*>(to)[1] = unpack8<CF_F16>(codes.y, scale);
+    reinterpret_cast<uint4*>(to)[2] = unpack8<CF_F16>(codes.z, scale);
+    reinterpret_cast<uint4*>(to)[3] = unpack8<CF_F16>(codes.w, scale);
 }
 
 // What the passes of a wavefront on its own need of the kernel around them.
@@ -478,8 +489,12 @@ __device__ __forceinline__ QueryPart query_part(const AttnArgs& a, const WavePla
     return load_query(static_cast<const uint16_t*>(a.q) + w.q_first + (int64_t)row * kD, st.trow[rb] >= 0, w.lg);
 }
 
-// The second pass over a run: the tiles whose scales do not fit fp16, with keys as codes, the query in three e4m3 terms and values and
-// probabilities in bf16, the latter as value and remainder.  The segments' slots hold sums already.
+// The scale of a row of queries in the second pass, where keys have any scale: between its largest channel and 2^-9 there is room for keys
+// up to 2^127 and down to 2^-117.
+constexpr int kOddScale = 16;
+
+// The second pass over a run: the tiles whose scales do not fit fp16, in bf16: queries of three terms, probabilities as value and remainder.
+// The segments' slots hold sums already.
 template <int DT, int PAIRING, int NRB, class Table>
 __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, const Table& tbl, const WavePlace& w, Rows<NRB>& st) {
     st.emit(w.massml, w.rows_wg, w.ss, false, w.li, w.lg);
@@ -491,29 +506,58 @@ __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, co
         if (d.ntok <= 0) break;
         TileRegs r;
         load_tile(a, s, d, walk.c_tok, w.hkv, w.li, w.lg, r);
-        if (tile_fits(r, d.ntok, w.li)) continue;
+        if (tile_fits(r, d.ntok, w.li, w.lg)) continue;
         st.enter(d.seg, w.massml, w.rows_wg, w.ss, true, w.li, w.lg);
         put_angles(w.cs, lane, d.delta, w.my_freq, 1.f);
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                *reinterpret_cast<uint4*>(w.v_lds + (16 * tb + w.li) * kVRow + 64 * w.lg + 16 * c) = unpack8<CF_BF16>(r.v[tb][c], scale_of(r.vs[tb]));
+        for (int tb = 0; tb < 2; ++tb) {
+            uint4* const to = reinterpret_cast<uint4*>(w.v_lds + (16 * tb + w.li) * kVRow + 64 * w.lg);
+            const float scale = scale_of(r.vs[tb]);
+            to[0] = unpack8<CF_BF16>(r.v[tb].x, scale);
+            to[1] = unpack8<CF_BF16>(r.v[tb].y, scale);
+            to[2] = unpack8<CF_BF16>(r.v[tb].z, scale);
+            to[3] = unpack8<CF_BF16>(r.v[tb].w, scale);
+        }
         wave_lds_order();
         f32x4 sc[NRB][2];
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
             const QueryPart q = query_part(a, w, st, rb);
-            const int scale = row_scale<DT>(q);
-            const Terms qt = to_terms<DT, PAIRING>(q, scale, w.cs, w.lg);
+            const int scale = min(row_scale<DT>(q) + kOddScale, 253);
+            const float down = scale_down(scale);
             sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = kTerms - 1; k >= 0; --k)    // the smallest terms first
+            for (int c = 0; c < 2; ++c) {            // channels 8c .. 8c + 7 of either half
+                float v[4][4];
+                turn4<DT, PAIRING>(q, 2 * c, w.cs, w.lg, v[0], v[2]);
+                turn4<DT, PAIRING>(q, 2 * c + 1, w.cs, w.lg, v[1], v[3]);
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) sc[rb][tb] = mma_fp4(r.k[tb], (int)r.ks[tb], qt.t[k], scale - 4 * k, sc[rb][tb]);
+                for (int h = 0; h < 2; ++h) {
+                    uint4 term[3];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x = v[2 * h + (i >> 1)][2 * (i & 1)] * down, y = v[2 * h + (i >> 1)][2 * (i & 1) + 1] * down;
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) {
+                            const uint32_t pair = Mma<CF_BF16>::pack(x, y);
+                            x -= Mma<CF_BF16>::lo(pair);
+                            y -= Mma<CF_BF16>::hi(pair);
+                            reinterpret_cast<uint32_t*>(&term[k])[i] = pair;
+                        }
+                    }
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        const uint4 kf = key_operand<CF_BF16>(r, tb, 2 * h + c, w.lg);
+#pragma unroll
+                        for (int k = 2; k >= 0; --k) sc[rb][tb] = Mma<CF_BF16>::run(kf, term[k], sc[rb][tb]);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
             const int lim = d.ntok - 4 * w.lg;
+            const float up = scale_of((uint32_t)scale);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
+            for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] * up : -INFINITY;
         }
         float pv[NRB][8];
         st.softmax(sc, [&](int) { return a.scale_log2e; }, pv);
@@ -524,16 +568,70 @@ __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, co
     st.cur_seg = -1;
 }
 
-// The run's tiles of the own block: 16-bit keys and values, queries and probabilities as value and remainder; row t sees tokens 0 .. t.
-template <int DT, int PAIRING, int NRB, class Table>
-__device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, const WavePlace& w, Rows<NRB>& st) {
+// Values of own tokens `odd` (a bit each) that are not finite, for the rows that see them (zero times one would reach the rows ahead).
+template <int DT, int NRB>
+__device__ __forceinline__ void add_odd_values(__amdgpu_buffer_rsrc_t values, int pitch, uint32_t odd, int tok0, int lg, Rows<NRB>& st) {
+    for (; odd; odd &= odd - 1) {
+        const int j = __builtin_ctz(odd);
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+            const auto x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(values, j * pitch + 32 * db + 8 * lg, 0, 0));
+            const float v[4] = {Mma<DT>::lo(x.x), Mma<DT>::hi(x.x), Mma<DT>::lo(x.y), Mma<DT>::hi(x.y)};
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (tok0 + j <= st.trow[rb] && !(fabsf(v[r]) < INFINITY)) st.acc[rb][db][r] += v[r];
+        }
+    }
+    st.pin();
+}
+
+// A tile of the own block: `ntok` keys (operands as in Parts, from key_at(tb, c)) and staged values; row t sees tokens 0 .. t.
+template <int DT, int NRB, class Key>
+__device__ __forceinline__ void own_tile(Rows<NRB>& st, const Parts (&qt)[NRB], Key key_at, const unsigned char* v_read, int tok0, int ntok, float mul, int lg) {
+    f32x4 sc[NRB][2];
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+            const uint4 kf = key_at(tb, c);
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) {
+                sc[rb][tb] = Mma<DT>::run(kf, qt[rb].lo[c], sc[rb][tb]);
+                sc[rb][tb] = Mma<DT>::run(kf, qt[rb].hi[c], sc[rb][tb]);
+            }
+        }
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+        const int last = min(ntok - 1, st.trow[rb] - tok0) - 4 * lg;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) <= last ? sc[rb][e >> 2][e & 3] : -INFINITY;
+    }
+    float pv[NRB][8];
+    st.softmax(sc, [&](int) { return mul; }, pv);
+    st.template weigh<DT, true>(v_read, pv);
+}
+
+// The scale of the queries against own keys: fp16 has to hold them turned, bf16 does already (and its keys take up the whole range).
+template <int DT>
+__device__ __forceinline__ int own_scale(int scale) { return DT == CF_F16 ? scale : 127; }
+
+// The run's tiles of the own block, for a wavefront on its own.
+template <int DT, int PAIRING, class Table>
+__device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, const WavePlace& w, Rows<1>& st) {
     const int lane = 16 * w.lg + w.li, li = w.li, lg = w.lg;
     RunWalk<true> walk(w.t_begin, w.t_end);
+    const QueryPart q = query_part(a, w, st, 0);
+    const int scale = own_scale<DT>(block_scale<DT>(q));
+    const float mul = a.scale_log2e * scale_of((uint32_t)scale);
     for (;;) {
         const Tile cd = walk.next(tbl, lane);
         if (cd.ntok <= 0) break;
         st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
-        put_angles(w.cs, lane, cd.delta, w.my_freq, 1.f);
+        put_angles(w.cs, lane, cd.delta, w.my_freq, scale_down(scale));
         const int64_t at = ((walk.c_tok + cd.tok0) * a.n_kv_heads + w.hkv) * kD * 2;
         const int pitch = a.n_kv_heads * kD * 2, range = (cd.ntok - 1) * pitch + 2 * kD;
         const auto rk = buffer(a.k_self, at, range), rv = buffer(a.v_self, at, range);
@@ -552,53 +650,10 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, c
             odd |= (uint32_t)((ballot | ballot >> 16 | ballot >> 32 | ballot >> 48) & 0xffff) << (16 * tb);
         }
         wave_lds_order();
-        f32x4 sc[NRB][2];
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            const QueryPart q = query_part(a, w, st, rb);
-            sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {            // channels 8c .. 8c + 7 of either half
-                float a0[4], b0[4], a1[4], b1[4];
-                turn4<DT, PAIRING>(q, 2 * c, w.cs, lg, a0, b0);
-                turn4<DT, PAIRING>(q, 2 * c + 1, w.cs, lg, a1, b1);
-                const float va[8] = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
-                const float vb[8] = {b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
-                uint4 ha, la, hb, lb;
-                split8<DT>(va, ha, la);
-                split8<DT>(vb, hb, lb);
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    sc[rb][tb] = Mma<DT>::run(kf[tb][c], la, sc[rb][tb]);
-                    sc[rb][tb] = Mma<DT>::run(kf[tb][2 + c], lb, sc[rb][tb]);
-                    sc[rb][tb] = Mma<DT>::run(kf[tb][c], ha, sc[rb][tb]);
-                    sc[rb][tb] = Mma<DT>::run(kf[tb][2 + c], hb, sc[rb][tb]);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            const int last = min(cd.ntok - 1, st.trow[rb] - cd.tok0) - 4 * lg;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) <= last ? sc[rb][e >> 2][e & 3] : -INFINITY;
-        }
-        float pv[NRB][8];
-        st.softmax(sc, [&](int) { return a.scale_log2e; }, pv);
-        st.template weigh<DT, true>(w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3), pv);
+        const Parts qt[1] = {to_parts<DT, PAIRING, DT>(q, w.cs, lg)};
+        own_tile<DT, 1>(st, qt, [&](int tb, int c) { return kf[tb][c]; }, w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3), cd.tok0, cd.ntok, mul, lg);
         wave_lds_order();                            // the next tile writes over what others read above
-        // values that are not finite, for the rows that see them (zero times one would reach the rows ahead)
-        for (; odd; odd &= odd - 1) {
-            const int j = __builtin_ctz(odd);
-#pragma unroll
-            for (int db = 0; db < 8; ++db) {
-                const auto x = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rv, j * pitch + 32 * db + 8 * lg, 0, 0));
-                const float v[4] = {Mma<DT>::lo(x.x), Mma<DT>::hi(x.x), Mma<DT>::lo(x.y), Mma<DT>::hi(x.y)};
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (cd.tok0 + j <= st.trow[rb] && !(fabsf(v[r]) < INFINITY)) st.acc[rb][db][r] += v[r];
-            }
-        }
-        st.pin();
+        add_odd_values<DT, 1>(rv, pitch, odd, cd.tok0, lg, st);
     }
 }
 
@@ -664,7 +719,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     fetch(d0, r0);
     fetch(d1, r1);
     const QueryPart q = query_part(a, w, st, 0);
-    const int q_scale = row_scale<DT>(q);
+    const int q_scale = block_scale<DT>(q);
     const float down = scale_down(q_scale), mul = a.scale_log2e * scale_of((uint32_t)q_scale);
     unsigned char* const v_write = w.v_lds + li * kVRow + 64 * lg;
     const unsigned char* const v_read = w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
@@ -674,33 +729,32 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     auto step = [&](Tile& d, TileRegs& r) __attribute__((always_inline)) {
         const Tile cd = d;
         // a tile that is passed over counts as one without tokens (no branch around the body: the compiler would keep the accumulators twice)
-        const bool take = tile_fits(r, cd.ntok, li);
+        const bool take = tile_fits(r, cd.ntok, li, lg);
         const int ntok = take ? cd.ntok : 0;
         passed_over = passed_over || !take;
         st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
         if (!have_parts || cd.delta != q_delta) {
             have_parts = true;
             q_delta = cd.delta;
-            put_angles(w.cs, lane, cd.delta, w.my_freq, 1.f);
-            qt = to_parts<DT, PAIRING>(q, down, w.cs, lg);
+            put_angles(w.cs, lane, cd.delta, w.my_freq, down);
+            qt = to_parts<DT, PAIRING, CF_F16>(q, w.cs, lg);
         }
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                *reinterpret_cast<uint4*>(v_write + 16 * tb * kVRow + 16 * c) = unpack8<CF_F16>(r.v[tb][c], take ? scale_of(r.vs[tb]) : 0.f);
+        for (int tb = 0; tb < 2; ++tb) stage_values(v_write + 16 * tb * kVRow, r.v[tb], take ? scale_of(r.vs[tb]) : 0.f);
         wave_lds_order();
         f32x4 sc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb) sc[0][tb] = mma_fp4(r.k[tb], (int)r.ks[tb], qt.lo, kLoScale, sc[0][tb]);
-#pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb) sc[0][tb] = Mma<CF_F16>::run(unpack8<CF_F16>(r.k[tb][c], take ? scale_of(r.ks[tb]) : 0.f), qt.hi[c], sc[0][tb]);
+            for (int tb = 0; tb < 2; ++tb) {
+                const uint4 kf = key_operand<CF_F16>(r, tb, c, lg);
+                sc[0][tb] = Mma<CF_F16>::run(kf, qt.lo[c], sc[0][tb]);
+                sc[0][tb] = Mma<CF_F16>::run(kf, qt.hi[c], sc[0][tb]);
+            }
         __builtin_amdgcn_sched_barrier(0);
         fetch(d, r);                                 // the registers are free again
         __builtin_amdgcn_sched_barrier(0);
-        if (ntok < kTile) {
+        if (ntok < kTile) {                          // (scores of a tile passed over are replaced as well)
             const int lim = ntok - 4 * lg;
 #pragma unroll
             for (int e = 0; e < 8; ++e) sc[0][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[0][e >> 2][e & 3] : -INFINITY;
@@ -716,9 +770,10 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
         if (d1.ntok <= 0) break;
         step(d1, r1);
     }
-    const bool own = walk.others;
     if (passed_over) with_table([&](const auto& t) __attribute__((always_inline)) { odd_tiles<DT, PAIRING, 1>(a, s, t, w, st); });
-    if (own) with_table([&](const auto& t) __attribute__((always_inline)) { own_tiles<DT, PAIRING, 1>(a, t, w, st); });
+    with_table([&](const auto& t) __attribute__((always_inline)) {
+        if (holds<true>(t, w.t_begin, w.t_end, lane)) own_tiles<DT, PAIRING>(a, t, w, st);
+    });
     st.emit(w.massml, w.rows_wg, w.ss, false, li, lg);
 
     // ---- the wavefronts' results: wavefront w merges channel block w
@@ -753,24 +808,31 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
 }
 
 // ---------------------------------------------------------------------------------------------
-// More row blocks: four wavefronts with NRB blocks each share 32-token tiles.  Bound by the instructions that a SIMD can issue.  Every thread
-// loads 8 bytes of a tile's key codes and of its value codes, three tiles ahead of their use; the key codes go to LDS as they are (a
-// wavefront unpacks them to its matrix operands), the values unpacked, each once per workgroup.  One barrier per tile.
-template <int DT, int PAIRING, int NRB>
-__global__ __launch_bounds__(kRowsThreads, NRB == 1 ? 3 : 2) void attn_q4_rows_kernel(AttnArgs a, RopeFreq freq, Plan p, Scales s) {
-    constexpr int kKBuf = kTile * kRowBytes;
+// More row blocks: eight wavefronts share the 32-token tiles that they stage together, two per step, one for each half of the workgroup to stage.
+// Bound by the instructions that a SIMD can issue.
+//   * HALVES (at most four blocks): a half streams a run of its own, wavefront w of it with block w; the halves meet in LDS at the end.
+//   * Otherwise the halves stage every other tile of one run and every wavefront works on both: NB0 blocks in the first half, NB1 in the
+//     second (a SIMD has a wavefront of either, so it gets NB0 + NB1).
+// A thread loads 8 bytes of a tile's key codes and of its value codes a step ahead of their staging, two ahead of their use, and unpacks them into
+// LDS, each once per workgroup, together with a description of the tile and the angles where a segment begins.  One barrier per step.
+template <int DT, int PAIRING, int NB0, int NB1, bool HALVES>
+__global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs a, RopeFreq freq, Plan p, Scales s) {
+    constexpr int kHalfWaves = kRowsWaves / 2, kHalfThreads = kRowsThreads / 2;
+    static_assert(!HALVES || (NB0 == 1 && NB1 == 1), "");
+    constexpr int kRowsWg = 16 * kHalfWaves * (HALVES ? 1 : NB0 + NB1);
     __shared__ SegTable tbl;
-    // two tiles' key codes, two of values, the workgroup's queries; after the last tile a V tile per wavefront
-    constexpr int kTiles = 2 * (kKBuf + kVTile), kQueries = kRowsWaves * NRB * 16 * kQRow;
-    constexpr int kRowsBytes = kTiles + kQueries > kRowsWaves * kVTile ? kTiles + kQueries : kRowsWaves * kVTile;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[kRowsBytes];
+    // tiles of keys and values, the workgroup's queries; after the last tile a V tile per wavefront, then the second half's results
+    constexpr int kKeys = 4 * kKTile, kTiles = kKeys + 4 * kVTile, kBytes = kTiles + kRowsWg * kQRow;
+    static_assert(kBytes >= kRowsWaves * kVTile && kBytes >= kHalfWaves * 8 * kWave * (int)sizeof(f32x4), "");
+    __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes];
     __shared__ __attribute__((aligned(16))) float2 cs_lds[kRowsWaves][64];
-    __shared__ uint32_t ks_lds[2][kTile];            // the keys' scale bytes, four of a token
-    __shared__ int odd_lds[2];                       // number of the last tile in a buffer whose scales do not fit fp16
+    __shared__ __attribute__((aligned(16))) int4 desc_lds[2][2];     // tokens, segment, shift and first token of a staged tile
+    __shared__ int odd_lds[2][2];                    // step of the last tile there whose scales do not fit fp16; own tiles: tokens with odd values
     __shared__ uint32_t top_lds;
+    __shared__ float2 red_ml[HALVES ? kRowsWg : 1];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), half = wave / kHalfWaves;
     const int li = lane & 15, lg = lane >> 4;
     // grid (split, kv head * row groups + row group, query)
     const int split = blockIdx.x, b = blockIdx.z;
@@ -778,164 +840,246 @@ __global__ __launch_bounds__(kRowsThreads, NRB == 1 ? 3 : 2) void attn_q4_rows_k
     const int unit = b * p.units_per_b + (int)blockIdx.y;
     const QueryHead qh = load_query_head(a, b, tid);
     const int tq = max(min(qh.tq_raw, a.max_tq), 0);
-    const int row0 = rg * p.rows_wg;
+    const int row0 = rg * kRowsWg;
     const bool wg_rows = row0 < p.group * tq;        // workgroup-uniform
-    Rows<NRB> st;
-    st.begin(row0 + wave * NRB * 16, p.group * tq, p.group, a.n_q_heads, hkv, li);
     char* const ws = static_cast<char*>(a.workspace);
-    WavePlace w;
-    w.li = li; w.lg = lg; w.hkv = hkv; w.rows_wg = p.rows_wg; w.ss = split;
-    w.q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
-    w.my_freq = freq.rev[lane];
-    w.cs = cs_lds[wave];
-    w.v_lds = lds + wave * kVTile;
-    w.massml = a.mass ? reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * p.rows_wg + wave * NRB * 16 : nullptr;
-    // the power of two that the workgroup's queries are scaled down by
-    if (tid == 0) { top_lds = 0; odd_lds[0] = odd_lds[1] = -1; }
-    uint32_t top = 0;
-    unsigned char* const q_lds = lds + kTiles + (wave * NRB * 16 + li) * kQRow + 32 * lg;     // (a wavefront reads its own rows only)
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-        const QueryPart q = query_part(a, w, st, rb);
-        top = max(top, largest<DT>(q));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = q.w[i];
-    }
-    build_table(a, qh, &tbl, kTile);                 // (its barriers are after the line above)
-    atomicMax(&top_lds, top);
-    const int total = wg_rows ? tbl.tile0[tbl.n] : 0;
-    w.t_begin = run_begin(total, p.nsplit, split);
-    w.t_end = run_begin(total, p.nsplit, split + 1);
 
-    RunWalk<false> walk(w.t_begin, w.t_end);
-    const int row_bytes = (int)(a.store_ts >> 1), scale_bytes = (int)(a.store_ts >> 5);
-    const int st_tok = tid >> 3, st_part = tid & 7;  // token and 16 channels that the thread stages
-    struct Regs { uint2 k, v; uint32_t vs, ks; };
-    auto fetch = [&](Tile& d, Regs& r) __attribute__((always_inline)) {
-        d = walk.next(tbl, lane);
-        const bool any = d.ntok > 0;
-        const int64_t at = any ? (walk.c_tok + d.tok0) * a.store_ts + (int64_t)hkv * a.store_hs : 0;
-        const int codes = any ? (d.ntok - 1) * row_bytes + kRowBytes : 0, scales = any ? (d.ntok - 1) * scale_bytes + 4 : 0;
-        const int off = st_tok * row_bytes + 8 * st_part;
-        r.k = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(buffer(a.k_store, at >> 1, codes), off, 0, 0));
-        r.v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(buffer(a.v_store, at >> 1, codes), off, 0, 0));
-        r.vs = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(s.v, at >> 5, scales), st_tok * scale_bytes + (st_part >> 1), 0, 0);
-        r.ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(s.k, at >> 5, scales), (lane & 31) * scale_bytes, 0, 0);
-    };
-    auto stage = [&](const Tile& d, const Regs& r, int buf, int number) __attribute__((always_inline)) {
-        unsigned char* const k_buf = lds + buf * kKBuf;
-        unsigned char* const v_buf = lds + 2 * kKBuf + buf * kVTile;
-        *reinterpret_cast<uint2*>(k_buf + 8 * tid) = r.k;
-        const bool fits = fits_f16(r.vs);
-        const float sv = fits ? scale_of(r.vs) : 0.f;
-        unsigned char* const to = v_buf + st_tok * kVRow + 32 * st_part;
-        *reinterpret_cast<uint4*>(to) = unpack8<CF_F16>(r.v.x, sv);
-        *reinterpret_cast<uint4*>(to + 16) = unpack8<CF_F16>(r.v.y, sv);
-        if (tid < kTile) ks_lds[buf][tid] = r.ks;
-        const bool k_fits = fits_f16(r.ks & 255) && fits_f16(r.ks >> 8 & 255) && fits_f16(r.ks >> 16 & 255) && fits_f16(r.ks >> 24);
-        if ((!fits && st_tok < d.ntok) || (!k_fits && tid < d.ntok)) odd_lds[buf] = number;
-    };
+    auto body = [&](auto nrb) __attribute__((always_inline)) {
+        constexpr int NRB = decltype(nrb)::value;
+        // the wavefront's first row, counted from the workgroup's
+        const int wrow = HALVES ? 16 * (wave - half * kHalfWaves) : half == 0 ? 16 * NB0 * wave : 16 * (kHalfWaves * NB0 + NB1 * (wave - kHalfWaves));
+        Rows<NRB> st;
+        st.begin(row0 + wrow, p.group * tq, p.group, a.n_q_heads, hkv, li);
+        WavePlace w;
+        w.li = li; w.lg = lg; w.hkv = hkv; w.rows_wg = kRowsWg; w.ss = HALVES ? 2 * split + half : split;
+        w.q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
+        w.my_freq = freq.rev[lane];
+        w.cs = cs_lds[wave];
+        w.v_lds = lds + wave * kVTile;
+        w.massml = a.mass ? reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * kRowsWg + wrow : nullptr;
+        // the power of two that the workgroup's queries are scaled down by
+        if (tid == 0) top_lds = 0;
+        if (tid < 4) odd_lds[tid >> 1][tid & 1] = -1;
+        uint32_t top = 0;
+        unsigned char* const q_lds = lds + kTiles + (wrow + li) * kQRow + 32 * lg;
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            const QueryPart q = query_part(a, w, st, rb);
+            top = max(top, largest<DT>(q));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = q.w[i];
+        }
+        build_table(a, qh, &tbl, kTile);             // (its barriers are after the lines above)
+        atomicMax(&top_lds, top);
+        const int total = wg_rows ? tbl.tile0[tbl.n] : 0;
+        const int runs = HALVES ? 2 * p.nsplit : p.nsplit;
+        w.t_begin = run_begin(total, runs, w.ss);
+        w.t_end = run_begin(total, runs, w.ss + 1);
 
-    Tile dc, dn;
-    Regs r;
-    fetch(dc, r);
-    __syncthreads();                                 // top_lds
-    const int q_scale = scale_byte_of<DT>(top_lds);
-    const float down = scale_down(q_scale), mul = a.scale_log2e * scale_of((uint32_t)q_scale);
-    // two tables of angles, of the current and of the next segment's tiles, times `down`
-    int cs_slot = 0;
-    auto angles = [&](int slot, int delta) __attribute__((always_inline)) {
-        if (wave == 0) {
+        // a half takes the tiles of its own run, or every other one of the workgroup's
+        RunWalk<false> walk(w.t_begin, w.t_end);
+        if (!HALVES && half == 1) walk.skip(tbl, lane);
+        const int row_bytes = (int)(a.store_ts >> 1), scale_bytes = (int)(a.store_ts >> 5);
+        const int st_tok = (tid & (kHalfThreads - 1)) >> 3, st_part = tid & 7;       // token and 16 channels that the thread stages
+        struct Regs { uint2 k, v; uint32_t ks, vs; };
+        auto fetch = [&](Tile& d, Regs& r) __attribute__((always_inline)) {
+            d = walk.next(tbl, lane);
+            const bool any = d.ntok > 0;
+            const int64_t at = any ? (walk.c_tok + d.tok0) * a.store_ts + (int64_t)hkv * a.store_hs : 0;
+            if constexpr (!HALVES) walk.skip(tbl, lane);             // (the other half's)
+            const int codes = any ? (d.ntok - 1) * row_bytes + kRowBytes : 0, scales = any ? (d.ntok - 1) * scale_bytes + 4 : 0;
+            const int off = st_tok * row_bytes + 8 * st_part, soff = st_tok * scale_bytes + (st_part >> 1);
+            r.k = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(buffer(a.k_store, at >> 1, codes), off, 0, 0));
+            r.v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(buffer(a.v_store, at >> 1, codes), off, 0, 0));
+            r.ks = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(s.k, at >> 5, scales), soff, 0, 0);
+            r.vs = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(s.v, at >> 5, scales), soff, 0, 0);
+        };
+        float down = 0.f;
+        auto angles = [&](int slot, int delta, float scale) __attribute__((always_inline)) {
             const float2 c = rope_cos_sin_fast(delta, w.my_freq);
-            cs_lds[slot][lane] = make_float2(c.x * down, c.y * down);
-        }
-    };
-    angles(0, dc.delta);
-    stage(dc, r, 0, 0);
-    fetch(dn, r);
-    Parts qt[NRB];
-    int q_delta = 0, number = 0;
-    bool have_parts = false, passed_over = false;
-    const unsigned char* const v_read = lds + 2 * kKBuf + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
-    // Step: tile `dc` is in buffer `buf`; the one after it, dn, is on its way to registers since a step ago, from where it goes to the other
-    // buffer, and the next one is requested.  (Two sets of registers, two tiles ahead: the compiler waits for both at the loop's head.)
-    for (int buf = 0; dc.ntok > 0; buf ^= 1, ++number) {
-        __syncthreads();                             // tile `dc` is staged; every wavefront is done with the other buffer
-        const Tile cd = dc;
-        const bool turn_next = dn.ntok > 0 && dn.delta != cd.delta;
-        const int next_delta = dn.delta;
-        dc = dn;
-        stage(dn, r, buf ^ 1, number + 1);
-        fetch(dn, r);
-        const bool take = odd_lds[buf] != number;
-        i32x4 kc[2];
-        uint32_t ks[2];
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb) {
-            kc[tb] = *reinterpret_cast<const i32x4*>(lds + buf * kKBuf + (16 * tb + li) * kRowBytes + 16 * lg);
-            ks[tb] = reinterpret_cast<const uint8_t*>(ks_lds[buf])[4 * (16 * tb + li) + lg];
-        }
-        st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
-        if (!have_parts || cd.delta != q_delta) {
-            have_parts = true;
-            q_delta = cd.delta;
+            cs_lds[slot][lane] = make_float2(c.x * scale, c.y * scale);
+        };
+        // tile d, loaded to r, to buffer `buf`; the first of a segment or run with its angles, which the half's wavefronts take turns in
+        auto stage = [&](const Tile& d, const Regs& r, int buf, int step, bool first) __attribute__((always_inline)) {
+            const bool fits = fits_f16(r.ks) && fits_f16(r.vs);
+            const float sk = scale_of(r.ks), sv = fits_f16(r.vs) ? scale_of(r.vs) : 0.f;
+            unsigned char* const k_to = lds + (2 * buf + half) * kKTile + st_tok * kKRow + 32 * st_part;
+            unsigned char* const v_to = lds + kKeys + (2 * buf + half) * kVTile + st_tok * kVRow + 32 * st_part;
+            *reinterpret_cast<uint4*>(k_to) = unpack8<CF_F16>(r.k.x, sk);
+            *reinterpret_cast<uint4*>(k_to + 16) = unpack8<CF_F16>(r.k.y, sk);
+            *reinterpret_cast<uint4*>(v_to) = unpack8<CF_F16>(r.v.x, sv);
+            *reinterpret_cast<uint4*>(v_to + 16) = unpack8<CF_F16>(r.v.y, sv);
+            if (!fits && st_tok < d.ntok) odd_lds[buf][half] = step;
+            if ((tid & (kHalfThreads - 1)) == 0) desc_lds[buf][half] = make_int4(d.ntok, d.seg, d.delta, d.tok0);
+            if ((first || d.tok0 == 0) && ((wave ^ step) & (kHalfWaves - 1)) == 0) angles(2 * buf + half, d.delta, down);
+        };
+        auto scalar = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
+        Parts qt[NRB];
+        auto turn = [&](auto type, int slot) __attribute__((always_inline)) {
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) {
                 QueryPart q;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) q.w[i] = *reinterpret_cast<const uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1));
-                qt[rb] = to_parts<DT, PAIRING>(q, 1.f, cs_lds[cs_slot], lg);
+                qt[rb] = to_parts<DT, PAIRING, decltype(type)::value>(q, cs_lds[slot], lg);
+            }
+        };
+
+        Tile dn;
+        Regs r;
+        fetch(dn, r);
+        __syncthreads();                             // top_lds
+        const int q_scale = scale_byte_of<DT>(top_lds);
+        down = scale_down(q_scale);
+        const float mul = a.scale_log2e * scale_of((uint32_t)q_scale);
+        stage(dn, r, 0, 0, true);
+        fetch(dn, r);
+        int q_delta = 0, step = 0;
+        bool have_parts = false, passed_over = false;
+        const unsigned char* const k_read = lds + li * kKRow + 32 * lg;
+        const unsigned char* const v_read = lds + kKeys + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
+        for (int buf = 0;; buf ^= 1, ++step) {
+            __syncthreads();                         // the step's tiles are staged; every wavefront is done with the other buffer
+            const int4 e0 = desc_lds[buf][0], e1 = desc_lds[buf][1];
+            if (scalar(e0.x | e1.x) == 0) break;
+            stage(dn, r, buf ^ 1, step + 1, false);
+            fetch(dn, r);
+            const int t_end = HALVES ? half + (scalar(half ? e1.x : e0.x) > 0) : 1 + (scalar(e1.x) > 0);
+#pragma unroll 1
+            for (int t = HALVES ? half : 0; t < t_end; ++t) {
+                const int slot = 2 * buf + t;
+                const int all = scalar(t ? e1.x : e0.x), seg = scalar(t ? e1.y : e0.y), delta = scalar(t ? e1.z : e0.z);
+                // a tile that is passed over counts as one without tokens (no branch around the body: the compiler would keep the accumulators twice)
+                const bool take = scalar(odd_lds[buf][t]) != step;
+                const int ntok = take ? all : 0;
+                passed_over = passed_over || !take;
+                st.enter(seg, w.massml, kRowsWg, w.ss, false, li, lg);
+                if (!have_parts || delta != q_delta) {
+                    have_parts = true;
+                    q_delta = delta;
+                    turn(std::integral_constant<int, CF_F16>{}, slot);
+                }
+                f32x4 sc[NRB][2];
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb) sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        const uint4 kf = *reinterpret_cast<const uint4*>(k_read + slot * kKTile + 16 * tb * kKRow + 128 * (c >> 1) + 16 * (c & 1));
+#pragma unroll
+                        for (int rb = 0; rb < NRB; ++rb) {
+                            sc[rb][tb] = Mma<CF_F16>::run(kf, qt[rb].lo[c], sc[rb][tb]);
+                            sc[rb][tb] = Mma<CF_F16>::run(kf, qt[rb].hi[c], sc[rb][tb]);
+                        }
+                    }
+                if (ntok < kTile) {
+                    const int lim = ntok - 4 * lg;
+#pragma unroll
+                    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
+                }
+                float pv[NRB][8];
+                st.softmax(sc, [&](int) { return mul; }, pv);
+                st.template weigh<CF_F16, false>(v_read + slot * kVTile, pv);
             }
         }
-        if (turn_next) {
-            cs_slot ^= 1;
-            angles(cs_slot, next_delta);
-        }
-        const int ntok = take ? cd.ntok : 0;
-        passed_over = passed_over || !take;
-        f32x4 sc[NRB][2];
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb) sc[rb][tb] = mma_fp4(kc[tb], (int)ks[tb], qt[rb].lo, kLoScale, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-                const uint4 kf = unpack8<CF_F16>(kc[tb][c], scale_of(ks[tb]));
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) sc[rb][tb] = Mma<CF_F16>::run(kf, qt[rb].hi[c], sc[rb][tb]);
+        const int wg_begin = HALVES ? run_begin(total, runs, 2 * split) : w.t_begin, wg_end = HALVES ? run_begin(total, runs, 2 * split + 2) : w.t_end;
+        __syncthreads();                             // every wavefront is done with the tiles and their descriptions
+        if (holds<true>(tbl, wg_begin, wg_end, lane)) {
+            // the own block, two tiles of 16-bit keys and values per step
+            RunWalk<true> own(w.t_begin, w.t_end);
+            if (!HALVES && half == 1) own.skip(tbl, lane);
+            const int scale = own_scale<DT>(q_scale);
+            const float own_down = scale_down(scale), own_mul = a.scale_log2e * scale_of((uint32_t)scale);
+            const int pitch = a.n_kv_heads * kD * 2;
+            for (;;) {
+                const Tile d = own.next(tbl, lane);
+                const bool any = d.ntok > 0;
+                const int64_t at = any ? ((own.c_tok + d.tok0) * a.n_kv_heads + hkv) * kD * 2 : 0;
+                if constexpr (!HALVES) own.skip(tbl, lane);
+                const int range = any ? (d.ntok - 1) * pitch + 2 * kD : 0;
+                const auto rk = buffer(a.k_self, at, range), rv = buffer(a.v_self, at, range);
+                const int off = st_tok * pitch + 32 * st_part;
+                const uint4 k0 = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
+                const uint4 k1 = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, off + 16, 0, 0));
+                const uint4 v0 = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
+                const uint4 v1 = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, off + 16, 0, 0));
+                if ((wave & (kHalfWaves - 1)) == 0) angles(half, d.delta, own_down);
+                if ((tid & (kHalfThreads - 1)) == 0) { desc_lds[0][half] = make_int4(d.ntok, d.seg, d.delta, d.tok0); odd_lds[0][half] = 0; }
+                __syncthreads();
+                bool not_finite = false;
+                unsigned char* const k_to = lds + half * kKTile + st_tok * kKRow + 32 * st_part;
+                unsigned char* const v_to = lds + kKeys + half * kVTile + st_tok * kVRow + 32 * st_part;
+                reinterpret_cast<uint4*>(k_to)[0] = k0;
+                reinterpret_cast<uint4*>(k_to)[1] = k1;
+                reinterpret_cast<uint4*>(v_to)[0] = finite8<DT>(v0, not_finite);
+                reinterpret_cast<uint4*>(v_to)[1] = finite8<DT>(v1, not_finite);
+                if (not_finite) atomicOr(&odd_lds[0][half], 1 << st_tok);
+                __syncthreads();
+                const int4 e0 = desc_lds[0][0], e1 = desc_lds[0][1];
+                if (scalar(e0.x | e1.x) == 0) break;
+                const int t_end = HALVES ? half + (scalar(half ? e1.x : e0.x) > 0) : 1 + (scalar(e1.x) > 0);
+#pragma unroll 1
+                for (int t = HALVES ? half : 0; t < t_end; ++t) {
+                    const int ntok = scalar(t ? e1.x : e0.x), seg = scalar(t ? e1.y : e0.y), tok0 = scalar(t ? e1.w : e0.w);
+                    st.enter(seg, w.massml, kRowsWg, w.ss, false, li, lg);
+                    turn(std::integral_constant<int, DT>{}, t);
+                    own_tile<DT, NRB>(st, qt, [&](int tb, int c) {
+                        return *reinterpret_cast<const uint4*>(k_read + t * kKTile + 16 * tb * kKRow + 128 * (c >> 1) + 16 * (c & 1));
+                    }, v_read + t * kVTile, tok0, ntok, own_mul, lg);
+                    const uint32_t odd = (uint32_t)scalar(odd_lds[0][t]);
+                    if (odd) {
+                        const int64_t tok = scalar64(tbl.tok[seg]) + tok0;
+                        add_odd_values<DT, NRB>(buffer(a.v_self, (tok * a.n_kv_heads + hkv) * kD * 2, (ntok - 1) * pitch + 2 * kD), pitch, odd, tok0, lg, st);
+                    }
+                }
+                __syncthreads();                     // every wavefront is done with the tiles and their descriptions
             }
-        if (ntok < kTile) {
-            const int lim = ntok - 4 * lg;
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
+            __syncthreads();
         }
-        float pv[NRB][8];
-        st.softmax(sc, [&](int) { return mul; }, pv);
-        st.template weigh<CF_F16, false>(v_read + buf * kVTile, pv);
-    }
-    const bool own = walk.others;
-    __syncthreads();                                 // the buffers become the wavefronts' own
-    if (passed_over) odd_tiles<DT, PAIRING, NRB>(a, s, tbl, w, st);
-    if (own) own_tiles<DT, PAIRING, NRB>(a, tbl, w, st);
-    st.emit(w.massml, w.rows_wg, w.ss, false, li, lg);
-    st.close();
-    const int64_t part = (int64_t)unit * p.nsplit + split;
-    float2* const ml = reinterpret_cast<float2*>(ws + p.off_ml) + part * p.rows_wg + wave * NRB * 16;
-    float* const opart = reinterpret_cast<float*>(ws + p.off_opart) + (part * p.rows_wg + wave * NRB * 16) * kD;
+        if (passed_over) odd_tiles<DT, PAIRING, NRB>(a, s, tbl, w, st);
+        st.emit(w.massml, kRowsWg, w.ss, false, li, lg);
+        st.close();
+        if constexpr (HALVES) {                      // the second half's rows join the first's
+            f32x4* const red = reinterpret_cast<f32x4*>(lds) + (wave - half * kHalfWaves) * 8 * kWave + lane;
+            __syncthreads();
+            if (half == 1) {
+                if (lg == 0) red_ml[wrow + li] = make_float2(st.m_run[0], st.l_run[0]);
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-        const float l = st.l_run[rb], inv = l > 0.f ? 1.f / l : l;       // (a sum that is not a number stays one)
-        if (lg == 0) ml[16 * rb + li] = make_float2(st.m_run[rb], st.trow[rb] >= 0 ? l : 0.f);
-        if (st.trow[rb] < 0) continue;
+                for (int db = 0; db < 8; ++db) red[db * kWave] = st.acc[0][db];
+            }
+            __syncthreads();
+            if (half == 1) return;
+            const float2 o = red_ml[wrow + li];
+            const float m = fmaxf(st.m_run[0], o.x), ms = m == -INFINITY ? 0.f : m;
+            const float f = __builtin_amdgcn_exp2f(st.m_run[0] - ms), g = __builtin_amdgcn_exp2f(o.x - ms);
+            st.m_run[0] = m;
+            st.l_run[0] = st.l_run[0] * f + o.y * g;
 #pragma unroll
-        for (int db = 0; db < 8; ++db) {
-            if (p.direct_out) store_out<DT>(a, w.q_first, st.qrow[rb], db, lg, st.acc[rb][db] * inv);
-            else *reinterpret_cast<f32x4*>(opart + (16 * rb + li) * kD + 16 * db + 4 * lg) = st.acc[rb][db] * inv;
+            for (int db = 0; db < 8; ++db) st.acc[0][db] = st.acc[0][db] * f + red[db * kWave] * g;
         }
+        const int64_t part = (int64_t)unit * p.nsplit + split;
+        float2* const ml = reinterpret_cast<float2*>(ws + p.off_ml) + part * kRowsWg + wrow;
+        float* const opart = reinterpret_cast<float*>(ws + p.off_opart) + (part * kRowsWg + wrow) * kD;
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            const float l = st.l_run[rb], inv = l > 0.f ? 1.f / l : l;       // (a sum that is not a number stays one)
+            if (lg == 0) ml[16 * rb + li] = make_float2(st.m_run[rb], st.trow[rb] >= 0 ? l : 0.f);
+            if (st.trow[rb] < 0) continue;
+#pragma unroll
+            for (int db = 0; db < 8; ++db) {
+                if (p.direct_out) store_out<DT>(a, w.q_first, st.qrow[rb], db, lg, st.acc[rb][db] * inv);
+                else *reinterpret_cast<f32x4*>(opart + (16 * rb + li) * kD + 16 * db + 4 * lg) = st.acc[rb][db] * inv;
+            }
+        }
+    };
+    if constexpr (NB0 == NB1) {
+        body(std::integral_constant<int, NB0>{});
+    } else {                                         // (both bodies pass the same barriers: the steps are the workgroup's)
+        if (half == 0) body(std::integral_constant<int, NB0>{});
+        else body(std::integral_constant<int, NB1>{});
     }
 }
 
@@ -1010,7 +1154,7 @@ __global__ __launch_bounds__(256) void q4_mass_kernel(AttnArgs a, Plan p) {
             const int sub0 = run_of(total, nsub, ts), sub1 = run_of(total, nsub, te - 1);
             const int n_sub = sub1 - sub0 + 1;
             // items: unit, run, row; threads take rows of one (unit, run) side by side
-            const int rows = min(p.rows_wg, 256), per = 256 / rows;      // rows_wg is a power of two
+            const int rows = p.rows_wg <= 64 ? p.rows_wg : p.rows_wg <= 128 ? 128 : 256, per = 256 / rows;   // rows_wg is at most 256
             const int row = tid & (rows - 1), first = tid / rows;
             for (int i = first; i < p.units_per_b * n_sub; i += per) {
                 const int u = (int)div_exact((unsigned)i, (unsigned)n_sub), sub = sub0 + i - u * n_sub;
@@ -1018,7 +1162,7 @@ __global__ __launch_bounds__(256) void q4_mass_kernel(AttnArgs a, Plan p) {
                 if (run_begin(total, nsub, sub) >= run_begin(total, nsub, sub + 1)) continue;
                 const int rg = u - (int)div_exact((unsigned)u, (unsigned)p.n_rg) * p.n_rg;
                 const int64_t unit = (int64_t)b * p.units_per_b + u;
-                if (rg * p.rows_wg + row >= n_rows) continue;
+                if (row >= p.rows_wg || rg * p.rows_wg + row >= n_rows) continue;
                 const float2 v = reinterpret_cast<const float2*>(ws + p.off_massml)[(unit * p.slots + s + sub) * p.rows_wg + row];
                 const float2 r = reinterpret_cast<const float2*>(ws + p.off_ml)[unit * p.nsplit * p.rows_wg + row];
                 const float m = r.x == -INFINITY ? 0.f : r.x;
@@ -1065,10 +1209,14 @@ cf_status launch_attention_q4(const AttnArgs& a, const q4::Scales& sc, const Rop
         if (p.solo) {
             if (a.seg_stride <= kWave) hipLaunchKernelGGL((attn_q4_solo_kernel<DT, PAIRING, true>), grid, dim3(kSoloThreads), 0, s, a, f, p, sc);
             else hipLaunchKernelGGL((attn_q4_solo_kernel<DT, PAIRING, false>), grid, dim3(kSoloThreads), 0, s, a, f, p, sc);
-        } else if (p.nrb == 1) {
-            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 1>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
+        } else if (p.halves) {
+            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 1, 1, true>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
+        } else if (p.rows_wg == 128) {
+            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 1, 1, false>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
+        } else if (p.rows_wg == 192) {
+            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 2, 1, false>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
         } else {
-            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 2>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
+            hipLaunchKernelGGL((attn_q4_rows_kernel<DT, PAIRING, 2, 2, false>), grid, dim3(kRowsThreads), 0, s, a, f, p, sc);
         }
     };
     auto by_pairing = [&](auto dt) {

@@ -13,7 +13,7 @@ namespace cf {
 namespace q4 {
 
 constexpr int kSoloWaves = 8;       // wavefronts of attn_q4_solo_kernel's workgroups, each with tiles of its own
-constexpr int kRowsWaves = 4;       // of attn_q4_rows_kernel's, each with rows of its own
+constexpr int kRowsWaves = 8;       // of attn_q4_rows_kernel's, which share tiles
 constexpr int kD = 128;
 constexpr int kTile = 32;           // tokens per tile
 constexpr int kMaxSplit = 64;
@@ -22,7 +22,7 @@ constexpr int kMaxEntries = 256;    // table entries of a query
 struct Plan {
     int group;          // query heads per kv head
     int solo;           // attn_q4_solo_kernel (one 16-row block), else attn_q4_rows_kernel
-    int nrb;            // 16-row blocks of a wavefront
+    int halves;         // of the latter: the workgroup's halves have runs of their own
     int runs;           // runs of tiles per workgroup
     int rows_wg;        // rows a workgroup has room for
     int n_rg;           // row groups (workgroups side by side) per (query, kv head)
@@ -38,15 +38,25 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.group = n_q_heads / n_kv_heads;
     const int64_t blocks = ((int64_t)p.group * max_tq + 15) / 16;
     p.solo = blocks <= 1;
-    p.nrb = blocks > 4 ? 2 : 1;
-    p.runs = p.solo ? kSoloWaves : 1;
-    p.rows_wg = p.solo ? 16 : 16 * p.nrb * kRowsWaves;
-    p.n_rg = (int)std::max<int64_t>((16 * blocks + p.rows_wg - 1) / p.rows_wg, 1);
+    p.halves = !p.solo && blocks <= 4;
+    p.runs = p.solo ? kSoloWaves : p.halves ? 2 : 1;
+    p.rows_wg = p.solo ? 16 : 64;
+    auto groups = [&](int rows) { return std::max<int64_t>((16 * blocks + rows - 1) / rows, 1); };
+    if (blocks > 4) {
+        // A step of a SIMD costs what its two wavefronts do once each, about as much as 1.5 row blocks, and its rows_wg / 64 row blocks.
+        int64_t best = 0;
+        for (int rows = 256; rows >= 128; rows -= 64) {
+            const int64_t wgs = (int64_t)batch * n_kv_heads * groups(rows), rounds = wgs < 256 ? wgs : (wgs + 255) / 256 * 256;
+            const int64_t cost = rounds * (3 + 2 * rows / 64);
+            if (best == 0 || cost < best) { best = cost; p.rows_wg = rows; }
+        }
+    }
+    p.n_rg = (int)groups(p.rows_wg);
     p.units_per_b = n_kv_heads * p.n_rg;
     p.units = batch * p.units_per_b;
     const int64_t tiles = plan_tiles(seg_stride, max_kv_tokens);
-    const int64_t room = p.solo ? 256 : 512, least = p.solo ? 2 * p.runs : 4;
-    p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({room / std::max(p.units, 1), tiles / least, (int64_t)kMaxSplit}), 1);
+    const int64_t least = p.solo ? 2 * p.runs : 4;
+    p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({256 / std::max(p.units, 1), tiles / least, (int64_t)kMaxSplit}), 1);
     p.direct_out = p.nsplit == 1;
     p.slots = seg_stride + p.nsplit * p.runs;
     size_t off = 0;
