@@ -55,12 +55,43 @@ __device__ __forceinline__ int run_of(int total, int n, int x) {
     return (int)((((int64_t)x + 1) * n - 1) / total);
 }
 
+// A query's table in LDS, laid out for the walk: where a segment's tiles end, by kind (0: of the other kind, or empty), and its fields side by side.
+struct RunTable {
+    int4 row[kMaxEntries];      // first tile, past the last tile, visible tokens, shift
+    int64_t tok[kMaxEntries];   // first token in its tensor
+    int store_end[kMaxEntries], own_end[kMaxEntries];
+    int n, total;
+};
+// All threads of a workgroup of at least kMaxEntries call this.  tmp: of use until it returns.
+__device__ __forceinline__ void build_run_table(const AttnArgs& a, const QueryHead& qh, RunTable* t, SegTable* tmp) {
+    const int tid = threadIdx.x;
+    auto put = [&](int s, int first, int end, int vis, int delta, int self, int64_t tok) __attribute__((always_inline)) {
+        t->row[s] = make_int4(first, end, vis, delta);
+        t->tok[s] = tok;
+        t->store_end[s] = !self && vis > 0 ? end : 0;
+        t->own_end[s] = self && vis > 0 ? end : 0;
+    };
+    if (a.seg_stride <= kWave) {                     // the first wavefront's registers do
+        if (tid < kWave) {
+            const RegSegTable r = build_reg_table(a, qh, tid, kTile);
+            put(tid, r.t0, r.t1, tid < r.n ? r.vis : 0, r.delta, r.self, r.tok);
+            if (tid == 0) { t->n = r.n; t->total = r.total; }
+        }
+    } else {
+        build_table(a, qh, tmp, kTile);
+        const int n = tmp->n;
+        if (tid < n) put(tid, tmp->tile0[tid], tmp->tile0[tid + 1], tmp->vis[tid], tmp->delta[tid], tmp->self[tid], tmp->tok[tid]);
+        else if (tid < kMaxEntries) put(tid, 0, 0, 0, 0, 0, 0);
+        if (tid == 0) { t->n = n; t->total = tmp->tile0[n]; }
+    }
+    __syncthreads();
+}
+
 // The first segment of a kind (of the own block, or of the store) whose tiles reach past tile x; -1: none.  `prev`: a segment that is not behind it.
 template <bool OWN>
-__device__ __forceinline__ int find_kind(const SegTable& t, int x, int lane, int prev) {
+__device__ __forceinline__ int find_kind(const RunTable& t, int x, int lane, int prev) {
     for (int s0 = prev < 0 ? 0 : prev & ~(kWave - 1); s0 < t.n; s0 += kWave) {
-        const int idx = s0 + lane;
-        const uint64_t hit = __ballot(idx < t.n && t.tile0[idx + 1] > x && (t.self[idx] != 0) == OWN && t.vis[idx] > 0);
+        const uint64_t hit = __ballot((OWN ? t.own_end : t.store_end)[s0 + lane] > x);
         if (hit) return s0 + __builtin_ctzll(hit);
     }
     return -1;
@@ -70,16 +101,18 @@ __device__ __forceinline__ int find_kind(const RegSegTable& t, int x, int lane, 
     const uint64_t hit = __ballot(lane < t.n && t.t1 > x && (t.self != 0) == OWN && t.vis > 0);
     return hit ? __builtin_ctzll(hit) : -1;
 }
-__device__ __forceinline__ int first_tile(const SegTable& t, int s) { return __builtin_amdgcn_readfirstlane(t.tile0[s]); }
+__device__ __forceinline__ int first_tile(const RunTable& t, int s) { return __builtin_amdgcn_readfirstlane(t.row[s].x); }
 __device__ __forceinline__ int first_tile(const RegSegTable& t, int s) { return __builtin_amdgcn_readlane(t.t0, s); }
 struct SegFields { int first, end, vis, delta; int64_t tok; };
 __device__ __forceinline__ int64_t scalar64(int64_t x) {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)x >> 32));
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
-__device__ __forceinline__ SegFields fields(const SegTable& t, int s) {
+__device__ __forceinline__ SegFields fields(const RunTable& t, int s) {
     auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-    return {scalar(t.tile0[s]), scalar(t.tile0[s + 1]), scalar(t.vis[s]), scalar(t.delta[s]), scalar64(t.tok[s])};
+    const int4 row = t.row[s];
+    const int64_t tok = t.tok[s];
+    return {scalar(row.x), scalar(row.y), scalar(row.z), scalar(row.w), scalar64(tok)};
 }
 __device__ __forceinline__ SegFields fields(const RegSegTable& t, int s) {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)t.tok, s), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)t.tok >> 32), s);
@@ -228,14 +261,23 @@ __device__ __forceinline__ int row_scale(const QueryPart& q) {
     return scale_byte_of<DT>(top);
 }
 
+// the largest over the 64 lanes
+__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
+    auto step = [](uint32_t x, auto ctrl, auto rows) {
+        return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+    };
+    using std::integral_constant;
+    v = step(v, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});     // row_shr:1, :2, :4, :8
+    v = step(v, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+    v = step(v, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+    v = step(v, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+    v = step(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});     // row_bcast:15, :31
+    v = step(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, kWave - 1);
+}
 // the same for the block as a whole
 template <int DT>
-__device__ __forceinline__ int block_scale(const QueryPart& q) {
-    uint32_t top = largest<DT>(q);
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    return __builtin_amdgcn_readfirstlane(scale_byte_of<DT>(top));
-}
+__device__ __forceinline__ int block_scale(const QueryPart& q) { return scale_byte_of<DT>(wave_top(largest<DT>(q))); }
 
 __device__ __forceinline__ float scale_down(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
 
@@ -243,7 +285,7 @@ __device__ __forceinline__ float scale_down(int scale) { return __uint_as_float(
 template <int DT>
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
     hi = Mma<DT>::pack(x, y);
-    lo = Mma<DT>::pack(x - Mma<DT>::lo(hi), y - Mma<DT>::hi(hi));
+    lo = Mma<DT>::pack(fmaf(Mma<DT>::lo(hi), -1.f, x), fmaf(Mma<DT>::hi(hi), -1.f, y));
 }
 template <int DT>
 __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
@@ -286,6 +328,20 @@ __device__ __forceinline__ uint4 finite8(uint4 v, bool& any) {
         w[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A staged tile of values, transposed: operand db holds channels 16 db .. + 15.
+struct Values { uint4 f[8]; };
+__device__ __forceinline__ Values load_values(const unsigned char* v_read) {
+    Values v;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) {
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(v_read + 32 * db));
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(v_read + 32 * db + 16 * kVRow));
+        const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+        v.f[db] = make_uint4(l2.x, l2.y, h2.x, h2.y);
+    }
+    return v;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -367,22 +423,18 @@ struct Rows {
             seg_l[rb] += lsum[rb];
         }
     }
-    // O^T += V^T P^T, V staged in the type VT.  EXACT: P as value and remainder.
+    // O^T += V^T P^T, V of the type VT.  EXACT: P as value and remainder.
     template <int VT, bool EXACT>
-    __device__ __forceinline__ void weigh(const unsigned char* v_read, const float (&pv)[NRB][8]) {
+    __device__ __forceinline__ void weigh(const Values& v, const float (&pv)[NRB][8]) {
         uint4 ph[NRB], pl[NRB];
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) split8<VT>(pv[rb], ph[rb], pl[rb]);
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
-            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(v_read + 32 * db));
-            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(v_read + 32 * db + 16 * kVRow));
-            const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-            const uint4 va = make_uint4(l2.x, l2.y, h2.x, h2.y);
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) {
-                if constexpr (EXACT) acc[rb][db] = Mma<VT>::run(va, pl[rb], acc[rb][db]);
-                acc[rb][db] = Mma<VT>::run(va, ph[rb], acc[rb][db]);
+                if constexpr (EXACT) acc[rb][db] = Mma<VT>::run(v.f[db], pl[rb], acc[rb][db]);
+                acc[rb][db] = Mma<VT>::run(v.f[db], ph[rb], acc[rb][db]);
             }
         }
     }
@@ -561,7 +613,7 @@ __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, co
         }
         float pv[NRB][8];
         st.softmax(sc, [&](int) { return a.scale_log2e; }, pv);
-        st.template weigh<CF_BF16, true>(w.v_lds + (4 * w.lg + (w.li >> 2)) * kVRow + 8 * (w.li & 3), pv);
+        st.template weigh<CF_BF16, true>(load_values(w.v_lds + (4 * w.lg + (w.li >> 2)) * kVRow + 8 * (w.li & 3)), pv);
         wave_lds_order();                            // the next tile writes over what others read above
     }
     st.emit(w.massml, w.rows_wg, w.ss, true, w.li, w.lg);
@@ -612,7 +664,7 @@ __device__ __forceinline__ void own_tile(Rows<NRB>& st, const Parts (&qt)[NRB], 
     }
     float pv[NRB][8];
     st.softmax(sc, [&](int) { return mul; }, pv);
-    st.template weigh<DT, true>(v_read, pv);
+    st.template weigh<DT, true>(load_values(v_read), pv);
 }
 
 // The scale of the queries against own keys: fp16 has to hold them turned, bf16 does already (and its keys take up the whole range).
@@ -669,11 +721,11 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t q_first, in
 // tiles ahead in registers; a tile's codes meet the query in registers, its values pass through LDS of the wavefront's own.
 template <int DT, int PAIRING, bool REG_TABLE>
 __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs a, RopeFreq freq, Plan p, Scales s) {
-    __shared__ std::conditional_t<REG_TABLE, int, SegTable> lds_tbl;
+    __shared__ std::conditional_t<REG_TABLE, int, RunTable> lds_tbl;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kSoloWaves * kVTile];
     __shared__ __attribute__((aligned(16))) float2 cs_lds[kSoloWaves][64];
     __shared__ float2 red_ml[kSoloWaves][16];
-    static_assert(kSoloWaves * kVTile >= kSoloWaves * 8 * kWave * (int)sizeof(f32x4), "the results reuse the V tiles");
+    static_assert(sizeof(lds) >= kSoloWaves * 8 * kWave * sizeof(f32x4) && sizeof(lds) >= sizeof(SegTable), "the results and the table reuse the V tiles");
 
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -691,8 +743,8 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
         rtbl = build_reg_table(a, qh, lane, kTile);
         total = rtbl.total;
     } else {
-        build_table(a, qh, &lds_tbl, kTile);
-        total = lds_tbl.tile0[lds_tbl.n];
+        build_run_table(a, qh, &lds_tbl, reinterpret_cast<SegTable*>(lds));
+        total = lds_tbl.total;
     }
     char* const ws = static_cast<char*>(a.workspace);
     WavePlace w;
@@ -754,6 +806,8 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
         __builtin_amdgcn_sched_barrier(0);
         fetch(d, r);                                 // the registers are free again
         __builtin_amdgcn_sched_barrier(0);
+        const Values vf = load_values(v_read);
+        __builtin_amdgcn_sched_barrier(0);
         if (ntok < kTile) {                          // (scores of a tile passed over are replaced as well)
             const int lim = ntok - 4 * lg;
 #pragma unroll
@@ -761,7 +815,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
         }
         float pv[1][8];
         st.softmax(sc, [&](int) { return mul; }, pv);
-        st.template weigh<CF_F16, false>(v_read, pv);
+        st.template weigh<CF_F16, false>(vf, pv);
         wave_lds_order();                            // the next step writes over what others read above
     };
     // (left from the middle: with a step skipped the wait for one register set would have to cover the other as well)
@@ -820,15 +874,15 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
     constexpr int kHalfWaves = kRowsWaves / 2, kHalfThreads = kRowsThreads / 2;
     static_assert(!HALVES || (NB0 == 1 && NB1 == 1), "");
     constexpr int kRowsWg = 16 * kHalfWaves * (HALVES ? 1 : NB0 + NB1);
-    __shared__ SegTable tbl;
+    __shared__ RunTable tbl;
     // tiles of keys and values, the workgroup's queries; after the last tile a V tile per wavefront, then the second half's results
     constexpr int kKeys = 4 * kKTile, kTiles = kKeys + 4 * kVTile, kBytes = kTiles + kRowsWg * kQRow;
-    static_assert(kBytes >= kRowsWaves * kVTile && kBytes >= kHalfWaves * 8 * kWave * (int)sizeof(f32x4), "");
+    static_assert(kBytes >= kRowsWaves * kVTile && kBytes >= kHalfWaves * 8 * kWave * (int)sizeof(f32x4) && kTiles >= (int)sizeof(SegTable), "");
     __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes];
     __shared__ __attribute__((aligned(16))) float2 cs_lds[kRowsWaves][64];
     __shared__ __attribute__((aligned(16))) int4 desc_lds[2][2];     // tokens, segment, shift and first token of a staged tile
     __shared__ int odd_lds[2][2];                    // step of the last tile there whose scales do not fit fp16; own tiles: tokens with odd values
-    __shared__ uint32_t top_lds;
+    __shared__ __attribute__((aligned(16))) uint4 top_lds[kRowsWaves / 4];
     __shared__ float2 red_ml[HALVES ? kRowsWg : 1];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -858,7 +912,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
         w.v_lds = lds + wave * kVTile;
         w.massml = a.mass ? reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * kRowsWg + wrow : nullptr;
         // the power of two that the workgroup's queries are scaled down by
-        if (tid == 0) top_lds = 0;
         if (tid < 4) odd_lds[tid >> 1][tid & 1] = -1;
         uint32_t top = 0;
         unsigned char* const q_lds = lds + kTiles + (wrow + li) * kQRow + 32 * lg;
@@ -869,9 +922,9 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
 #pragma unroll
             for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = q.w[i];
         }
-        build_table(a, qh, &tbl, kTile);             // (its barriers are after the lines above)
-        atomicMax(&top_lds, top);
-        const int total = wg_rows ? tbl.tile0[tbl.n] : 0;
+        reinterpret_cast<uint32_t*>(top_lds)[wave] = wave_top(top);
+        build_run_table(a, qh, &tbl, reinterpret_cast<SegTable*>(lds));              // (its barriers are after the lines above)
+        const int total = wg_rows ? __builtin_amdgcn_readfirstlane(tbl.total) : 0;
         const int runs = HALVES ? 2 * p.nsplit : p.nsplit;
         w.t_begin = run_begin(total, runs, w.ss);
         w.t_end = run_begin(total, runs, w.ss + 1);
@@ -928,8 +981,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
         Tile dn;
         Regs r;
         fetch(dn, r);
-        __syncthreads();                             // top_lds
-        const int q_scale = scale_byte_of<DT>(top_lds);
+        const uint4 t0 = top_lds[0], t1 = top_lds[1];
+        const int q_scale = scale_byte_of<DT>((uint32_t)scalar((int)max(max(max(t0.x, t0.y), max(t0.z, t0.w)), max(max(t1.x, t1.y), max(t1.z, t1.w)))));
         down = scale_down(q_scale);
         const float mul = a.scale_log2e * scale_of((uint32_t)q_scale);
         stage(dn, r, 0, 0, true);
@@ -962,17 +1015,26 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                 f32x4 sc[NRB][2];
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb) sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                // (all of a tile's operands are asked for ahead of the products: else the compiler waits for each)
+                uint4 kf[4][2];
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        const uint4 kf = *reinterpret_cast<const uint4*>(k_read + slot * kKTile + 16 * tb * kKRow + 128 * (c >> 1) + 16 * (c & 1));
+                    for (int tb = 0; tb < 2; ++tb)
+                        kf[c][tb] = *reinterpret_cast<const uint4*>(k_read + slot * kKTile + 16 * tb * kKRow + 128 * (c >> 1) + 16 * (c & 1));
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                         for (int rb = 0; rb < NRB; ++rb) {
-                            sc[rb][tb] = Mma<CF_F16>::run(kf, qt[rb].lo[c], sc[rb][tb]);
-                            sc[rb][tb] = Mma<CF_F16>::run(kf, qt[rb].hi[c], sc[rb][tb]);
+                            sc[rb][tb] = Mma<CF_F16>::run(kf[c][tb], qt[rb].lo[c], sc[rb][tb]);
+                            sc[rb][tb] = Mma<CF_F16>::run(kf[c][tb], qt[rb].hi[c], sc[rb][tb]);
                         }
-                    }
+                __builtin_amdgcn_sched_barrier(0);
+                const Values vf = load_values(v_read + slot * kVTile);
+                __builtin_amdgcn_sched_barrier(0);
                 if (ntok < kTile) {
                     const int lim = ntok - 4 * lg;
 #pragma unroll
@@ -982,7 +1044,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                 }
                 float pv[NRB][8];
                 st.softmax(sc, [&](int) { return mul; }, pv);
-                st.template weigh<CF_F16, false>(v_read + slot * kVTile, pv);
+                st.template weigh<CF_F16, false>(vf, pv);
             }
         }
         const int wg_begin = HALVES ? run_begin(total, runs, 2 * split) : w.t_begin, wg_end = HALVES ? run_begin(total, runs, 2 * split + 2) : w.t_end;
