@@ -37,7 +37,7 @@ using attn::wave_lds_order;
 
 namespace {
 
-constexpr int kSoloThreads = kSoloWaves * kWave, kRowsThreads = kRowsWaves * kWave;
+constexpr int kSoloThreads = kSoloWaves * kWave, kRowsThreads = kRowsWaves * kWave, kMassThreads = 1024;
 constexpr int kKRow = 272, kVRow = 288;              // bytes per token of a staged tile
 constexpr int kKTile = kTile * kKRow, kVTile = kTile * kVRow;
 constexpr int kRowBytes = 64;                        // codes of a row
@@ -1198,53 +1198,85 @@ __global__ __launch_bounds__(256) void q4_combine_kernel(AttnArgs a, Plan p) {
 
 // Per-segment attention mass, a workgroup per table entry: over the units, the runs that hold the segment's tiles and the rows, sum * exp2(reference -
 // row maximum) / row sum, in a fixed order.  Then S += mass (Alg. 2): a document slot's first entry works out the masses of all of the slot's
-// entries and adds them up in table order.
-__global__ __launch_bounds__(256) void q4_mass_kernel(AttnArgs a, Plan p) {
+// entries and adds them up in table order.  Bound by latency: the pairs of several items are asked for at once.
+__global__ __launch_bounds__(kMassThreads) void q4_mass_kernel(AttnArgs a, Plan p) {
     __shared__ SegTable tbl;
-    __shared__ float part_sum[4];
-    const int b = blockIdx.y, entry = blockIdx.x, tid = threadIdx.x;
-    const QueryHead qh = load_query_head(a, b, tid);
-    build_table(a, qh, &tbl, kTile);
-    if (entry >= tbl.n) return;
+    __shared__ float part_sum[kMassThreads / kWave];
+    const int b = blockIdx.y, entry = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1);
+    const bool in_regs = a.seg_stride <= kWave;      // every wavefront keeps the table in registers
+    const QueryHead qh = load_query_head(a, b, in_regs ? lane : tid);
+    RegSegTable reg;
+    if (in_regs) reg = build_reg_table(a, qh, lane, kTile);
+    else build_table(a, qh, &tbl, kTile);
+    const int n = in_regs ? reg.n : tbl.n, total = in_regs ? reg.total : tbl.tile0[tbl.n];
+    if (entry >= n) return;
+    auto doc_of = [&](int s) { return in_regs ? __builtin_amdgcn_readlane(qh.seg.doc, s) : tbl.doc[s]; };
     const char* ws = static_cast<const char*>(a.workspace);
     const int tq = max(min(qh.tq_raw, a.max_tq), 0), n_rows = p.group * tq;
-    const int total = tbl.tile0[tbl.n], nsub = p.nsplit * p.runs;
+    const int nsub = p.nsplit * p.runs;
+    // items: unit, run, row; threads take rows of one (unit, run) side by side
+    const int rows = p.rows_wg <= 16 ? 16 : p.rows_wg <= 64 ? 64 : p.rows_wg <= 128 ? 128 : 256, per = (int)blockDim.x / rows;
+    const int row = tid & (rows - 1), first = tid / rows;
+    const float inv_rg = 1.f / (float)p.n_rg, inv_nsub = 1.f / (float)nsub;
     auto mass_of = [&](int s) {
-        const int ts = tbl.tile0[s], te = tbl.tile0[s + 1];
+        const int ts = in_regs ? __builtin_amdgcn_readlane(reg.t0, s) : tbl.tile0[s], te = in_regs ? __builtin_amdgcn_readlane(reg.t1, s) : tbl.tile0[s + 1];
         float sum = 0.f;
         if (te > ts) {
             const int sub0 = run_of(total, nsub, ts), sub1 = run_of(total, nsub, te - 1);
-            const int n_sub = sub1 - sub0 + 1;
-            // items: unit, run, row; threads take rows of one (unit, run) side by side
-            const int rows = p.rows_wg <= 64 ? p.rows_wg : p.rows_wg <= 128 ? 128 : 256, per = 256 / rows;   // rows_wg is at most 256
-            const int row = tid & (rows - 1), first = tid / rows;
-            for (int i = first; i < p.units_per_b * n_sub; i += per) {
-                const int u = (int)div_exact((unsigned)i, (unsigned)n_sub), sub = sub0 + i - u * n_sub;
-                // a run between a segment's first and last may own no tile at all: its slot was not written
-                if (run_begin(total, nsub, sub) >= run_begin(total, nsub, sub + 1)) continue;
-                const int rg = u - (int)div_exact((unsigned)u, (unsigned)p.n_rg) * p.n_rg;
-                const int64_t unit = (int64_t)b * p.units_per_b + u;
-                if (row >= p.rows_wg || rg * p.rows_wg + row >= n_rows) continue;
-                const float2 v = reinterpret_cast<const float2*>(ws + p.off_massml)[(unit * p.slots + s + sub) * p.rows_wg + row];
-                const float2 r = reinterpret_cast<const float2*>(ws + p.off_ml)[unit * p.nsplit * p.rows_wg + row];
-                const float m = r.x == -INFINITY ? 0.f : r.x;
-                sum += v.y * __builtin_amdgcn_exp2f(v.x - m) * (r.y > 0.f ? 1.f / r.y : r.y);
+            const int n_sub = sub1 - sub0 + 1, items = p.units_per_b * n_sub;
+            const float2* const pairs = reinterpret_cast<const float2*>(ws + p.off_massml) + ((int64_t)b * p.units_per_b * p.slots + s + sub0) * p.rows_wg + row;
+            const float2* const whole = reinterpret_cast<const float2*>(ws + p.off_ml) + (int64_t)b * p.units_per_b * p.nsplit * p.rows_wg + row;
+            constexpr int kBatch = 8;
+            // item first + k * per as (unit, run), stepped without a division; fewer than 2^21 units
+            const float inv_sub = 1.f / (float)n_sub;
+            const int du = (int)div_small((unsigned)per, (unsigned)n_sub, inv_sub), ds = per - du * n_sub;
+            int u = (int)div_small((unsigned)first, (unsigned)n_sub, inv_sub), sub = first - u * n_sub;
+            for (int left = items - first; left > 0; left -= kBatch * per) {
+                float2 v[kBatch], r[kBatch];
+                bool take[kBatch];
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) {
+                    const int rg = p.n_rg == 1 ? 0 : u - (int)div_small((unsigned)u, (unsigned)p.n_rg, inv_rg) * p.n_rg;
+                    take[j] = j * per < left && row < p.rows_wg && rg * p.rows_wg + row < n_rows;
+                    // a run between a segment's first and last may own no tile at all: its slot was not written
+                    if (total < nsub) {
+                        const unsigned at = (unsigned)(total * (sub0 + sub));
+                        take[j] = take[j] && div_small(at, (unsigned)nsub, inv_nsub) < div_small(at + (unsigned)total, (unsigned)nsub, inv_nsub);
+                    }
+                    v[j] = r[j] = make_float2(0.f, 0.f);
+                    if (take[j]) {
+                        v[j] = pairs[((int64_t)u * p.slots + sub) * p.rows_wg];
+                        r[j] = whole[(int64_t)u * p.nsplit * p.rows_wg];
+                    }
+                    u += du;
+                    sub += ds;
+                    if (sub >= n_sub) { sub -= n_sub; ++u; }
+                }
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) {
+                    const float m = r[j].x == -INFINITY ? 0.f : r[j].x;
+                    if (take[j]) sum += v[j].y * __builtin_amdgcn_exp2f(v[j].x - m) * (r[j].y > 0.f ? 1.f / r[j].y : r[j].y);
+                }
             }
         }
-        sum = wave_sum(sum);
+        sum = wave_sum_dpp(sum);
         __syncthreads();
-        if ((tid & (kWave - 1)) == 0) part_sum[tid / kWave] = sum;
+        if (lane == 0) part_sum[tid / kWave] = sum;
         __syncthreads();
-        return ((part_sum[0] + part_sum[1]) + part_sum[2]) + part_sum[3];
+        float all = part_sum[0];
+#pragma unroll
+        for (int w = 1; w < kMassThreads / kWave; ++w)
+            if (w * kWave < (int)blockDim.x) all += part_sum[w];
+        return all;
     };
     const float mine = mass_of(entry);
     if (tid == 0) a.mass[(int64_t)b * a.seg_stride + entry] = mine;
     if (a.score_accum == nullptr) return;
-    const int d = tbl.doc[entry];
+    const int d = doc_of(entry);
     if (d < 0 || d >= a.score_stride) return;
     float sum = mine;
-    for (int j = 0; j < tbl.n; ++j) {                // workgroup-uniform
-        if (tbl.doc[j] != d) continue;
+    for (int j = 0; j < n; ++j) {                    // workgroup-uniform
+        if (doc_of(j) != d) continue;
         if (j < entry) return;
         if (j > entry) sum += mass_of(j);
     }
@@ -1296,7 +1328,7 @@ cf_status launch_attention_q4(const AttnArgs& a, const q4::Scales& sc, const Rop
         CF_HIP(hipGetLastError());
     }
     if (a.mass != nullptr) {
-        hipLaunchKernelGGL(q4_mass_kernel, dim3((unsigned)a.seg_stride, (unsigned)a.batch), dim3(256), 0, s, a, p);
+        hipLaunchKernelGGL(q4_mass_kernel, dim3((unsigned)a.seg_stride, (unsigned)a.batch), dim3((unsigned)p.mass_threads), 0, s, a, p);
         CF_HIP(hipGetLastError());
     }
     return CF_OK;

@@ -27,6 +27,7 @@ struct Plan {
     int rows_wg;        // rows a workgroup has room for
     int n_rg;           // row groups (workgroups side by side) per (query, kv head)
     int units_per_b, units, nsplit, slots;
+    int mass_threads;   // of a workgroup of q4_mass_kernel
     int direct_out;     // one split: the attention kernel writes the output rows itself
     size_t off_ml, off_opart, off_massml, total;
 };
@@ -43,11 +44,14 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.rows_wg = p.solo ? 16 : 64;
     auto groups = [&](int rows) { return std::max<int64_t>((16 * blocks + rows - 1) / rows, 1); };
     if (blocks > 4) {
-        // A step of a SIMD costs what its two wavefronts do once each, about as much as 1.5 row blocks, and its rows_wg / 64 row blocks.
+        p.rows_wg = 128;
+        // More workgroups than CUs: the fewest rounds' worth of work.  A step of a SIMD costs what its two wavefronts do once each, about as much
+        // as 1.5 row blocks, and its rows_wg / 64 row blocks.  (64 queries of 384 rows per kv head over 3000 tokens: 284 us with 128 rows, 189 with
+        // 192, 225 with 256.)  Fewer workgroups than that are split, and small ones leave fewer partial rows (448 rows x 4 kv heads x 7500
+        // tokens, with the merge: 41.0 us with 128 rows, 45.4 with 192, 45.7 with 256).
         int64_t best = 0;
-        for (int rows = 256; rows >= 128; rows -= 64) {
-            const int64_t wgs = (int64_t)batch * n_kv_heads * groups(rows), rounds = wgs < 256 ? wgs : (wgs + 255) / 256 * 256;
-            const int64_t cost = rounds * (3 + 2 * rows / 64);
+        for (int rows = 256; rows >= 128 && (int64_t)batch * n_kv_heads * groups(128) > 256; rows -= 64) {
+            const int64_t rounds = ((int64_t)batch * n_kv_heads * groups(rows) + 255) / 256, cost = rounds * (3 + 2 * rows / 64);
             if (best == 0 || cost < best) { best = cost; p.rows_wg = rows; }
         }
     }
@@ -58,6 +62,8 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     const int64_t least = p.solo ? 2 * p.runs : 4;
     p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({256 / std::max(p.units, 1), tiles / least, (int64_t)kMaxSplit}), 1);
     p.direct_out = p.nsplit == 1;
+    // few table entries: many threads for each, whose loads are out at once; many: no more than have an item each
+    p.mass_threads = (int64_t)batch * seg_stride > 512 ? 256 : 1024;
     p.slots = seg_stride + p.nsplit * p.runs;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
