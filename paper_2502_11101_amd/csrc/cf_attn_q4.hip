@@ -55,6 +55,16 @@ __device__ __forceinline__ int run_of(int total, int n, int x) {
     return (int)((((int64_t)x + 1) * n - 1) / total);
 }
 
+// The arguments that a kernel needs on its way to its first tile, asked for at once (the compiler would load each where it is first used, a round
+// trip every time).
+__device__ __forceinline__ void ask_for_arguments(const AttnArgs& a, const Plan& p, const Scales& s) {
+    const void *p0 = a.q, *p1 = a.q_off, *p2 = a.q_new_start, *p3 = a.k_store, *p4 = a.v_store, *p5 = s.k, *p6 = s.v, *p7 = a.segs, *p8 = a.n_seg,
+               *p9 = a.workspace, *p10 = a.mass, *p11 = a.k_self;
+    asm volatile("" ::"s"(p0), "s"(p1), "s"(p2), "s"(p3), "s"(p4), "s"(p5), "s"(p6), "s"(p7), "s"(p8), "s"(p9), "s"(p10), "s"(p11), "s"(a.n_store_tokens),
+                 "s"(a.seg_stride), "s"(a.batch), "s"(a.max_tq), "s"(a.n_q_heads), "s"(a.n_kv_heads), "s"(a.q_stored_start), "s"(a.store_ts),
+                 "s"(a.store_hs), "s"(a.max_positions), "s"(p.group), "s"(p.n_rg), "s"(p.nsplit), "s"(p.slots));
+}
+
 // A query's table in LDS, laid out for the walk: where a segment's tiles end, by kind (0: of the other kind, or empty), and its fields side by side.
 struct RunTable {
     int4 row[kMaxEntries];      // first tile, past the last tile, visible tokens, shift
@@ -62,7 +72,7 @@ struct RunTable {
     int store_end[kMaxEntries], own_end[kMaxEntries];
     int n, total;
 };
-// All threads of a workgroup of at least kMaxEntries call this.  tmp: of use until it returns.
+// All threads of a workgroup of at least kMaxEntries call this, and pass a barrier before they use the table or what tmp was made from.
 __device__ __forceinline__ void build_run_table(const AttnArgs& a, const QueryHead& qh, RunTable* t, SegTable* tmp) {
     const int tid = threadIdx.x;
     auto put = [&](int s, int first, int end, int vis, int delta, int self, int64_t tok) __attribute__((always_inline)) {
@@ -84,7 +94,6 @@ __device__ __forceinline__ void build_run_table(const AttnArgs& a, const QueryHe
         else if (tid < kMaxEntries) put(tid, 0, 0, 0, 0, 0, 0);
         if (tid == 0) { t->n = n; t->total = tmp->tile0[n]; }
     }
-    __syncthreads();
 }
 
 // The first segment of a kind (of the own block, or of the store) whose tiles reach past tile x; -1: none.  `prev`: a segment that is not behind it.
@@ -535,10 +544,10 @@ __device__ __forceinline__ void put_angles(float2* cs, int lane, int delta, doub
 }
 
 template <int NRB>
-__device__ __forceinline__ QueryPart query_part(const AttnArgs& a, const WavePlace& w, const Rows<NRB>& st, int rb) {
+__device__ __forceinline__ QueryPart query_part(const AttnArgs& a, int64_t q_first, const Rows<NRB>& st, int rb, int lg) {
     int row = st.qrow[rb];
     asm volatile("" : "+v"(row));                    // its addresses are worked out anew, not kept through the loops
-    return load_query(static_cast<const uint16_t*>(a.q) + w.q_first + (int64_t)row * kD, st.trow[rb] >= 0, w.lg);
+    return load_query(static_cast<const uint16_t*>(a.q) + q_first + (int64_t)row * kD, st.trow[rb] >= 0, lg);
 }
 
 // The scale of a row of queries in the second pass, where keys have any scale: between its largest channel and 2^-9 there is room for keys
@@ -574,7 +583,7 @@ __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, co
         f32x4 sc[NRB][2];
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
-            const QueryPart q = query_part(a, w, st, rb);
+            const QueryPart q = query_part(a, w.q_first, st, rb, w.lg);
             const int scale = min(row_scale<DT>(q) + kOddScale, 253);
             const float down = scale_down(scale);
             sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -673,36 +682,39 @@ __device__ __forceinline__ int own_scale(int scale) { return DT == CF_F16 ? scal
 
 // The run's tiles of the own block, for a wavefront on its own.
 template <int DT, int PAIRING, class Table>
-__device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, const WavePlace& w, Rows<1>& st) {
+__device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, const WavePlace& w, const QueryPart& q, int q_scale, Rows<1>& st) {
     const int lane = 16 * w.lg + w.li, li = w.li, lg = w.lg;
     RunWalk<true> walk(w.t_begin, w.t_end);
-    const QueryPart q = query_part(a, w, st, 0);
-    const int scale = own_scale<DT>(block_scale<DT>(q));
+    const int scale = own_scale<DT>(q_scale);
     const float mul = a.scale_log2e * scale_of((uint32_t)scale);
     for (;;) {
         const Tile cd = walk.next(tbl, lane);
         if (cd.ntok <= 0) break;
-        st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
-        put_angles(w.cs, lane, cd.delta, w.my_freq, scale_down(scale));
         const int64_t at = ((walk.c_tok + cd.tok0) * a.n_kv_heads + w.hkv) * kD * 2;
         const int pitch = a.n_kv_heads * kD * 2, range = (cd.ntok - 1) * pitch + 2 * kD;
         const auto rk = buffer(a.k_self, at, range), rv = buffer(a.v_self, at, range);
-        uint4 kf[2][4];
+        uint4 kf[2][4], vals[2][4];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                kf[tb][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, (16 * tb + li) * pitch + 32 * lg + 128 * (c >> 1) + 16 * (c & 1), 0, 0));
+                vals[tb][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, (16 * tb + li) * pitch + 64 * lg + 16 * c, 0, 0));
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
+        put_angles(w.cs, lane, cd.delta, w.my_freq, scale_down(scale));
+        const Parts qt[1] = {to_parts<DT, PAIRING, DT>(q, w.cs, lg)};
         uint32_t odd = 0;                            // tokens with values that are not finite
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
             bool any = false;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                kf[tb][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, (16 * tb + li) * pitch + 32 * lg + 128 * (c >> 1) + 16 * (c & 1), 0, 0));
-                const uint4 v = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, (16 * tb + li) * pitch + 64 * lg + 16 * c, 0, 0));
-                *reinterpret_cast<uint4*>(w.v_lds + (16 * tb + li) * kVRow + 64 * lg + 16 * c) = finite8<DT>(v, any);
-            }
+            for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4*>(w.v_lds + (16 * tb + li) * kVRow + 64 * lg + 16 * c) = finite8<DT>(vals[tb][c], any);
             const uint64_t ballot = __ballot(any);
             odd |= (uint32_t)((ballot | ballot >> 16 | ballot >> 32 | ballot >> 48) & 0xffff) << (16 * tb);
         }
         wave_lds_order();
-        const Parts qt[1] = {to_parts<DT, PAIRING, DT>(q, w.cs, lg)};
         own_tile<DT, 1>(st, qt, [&](int tb, int c) { return kf[tb][c]; }, w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3), cd.tok0, cd.ntok, mul, lg);
         wave_lds_order();                            // the next tile writes over what others read above
         add_odd_values<DT, 1>(rv, pitch, odd, cd.tok0, lg, st);
@@ -730,6 +742,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int li = lane & 15, lg = lane >> 4;
+    ask_for_arguments(a, p, s);
     // grid (split, kv head, query)
     const int split = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z;
     const int unit = b * p.units_per_b + hkv;
@@ -737,6 +750,8 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     const int tq = max(min(qh.tq_raw, a.max_tq), 0);
     Rows<1> st;
     st.begin(0, p.group * tq, p.group, a.n_q_heads, hkv, li);
+    const int64_t q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
+    const QueryPart q = query_part(a, q_first, st, 0, lg);           // (loads return in order: ahead of the tiles')
     RegSegTable rtbl;
     int total;
     if constexpr (REG_TABLE) {
@@ -744,6 +759,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
         total = rtbl.total;
     } else {
         build_run_table(a, qh, &lds_tbl, reinterpret_cast<SegTable*>(lds));
+        __syncthreads();
         total = lds_tbl.total;
     }
     char* const ws = static_cast<char*>(a.workspace);
@@ -751,7 +767,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     w.li = li; w.lg = lg; w.hkv = hkv; w.rows_wg = p.rows_wg; w.ss = split * kSoloWaves + wave;
     w.t_begin = run_begin(total, p.nsplit * kSoloWaves, w.ss);
     w.t_end = run_begin(total, p.nsplit * kSoloWaves, w.ss + 1);
-    w.q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
+    w.q_first = q_first;
     w.my_freq = freq.rev[lane];
     w.cs = cs_lds[wave];
     w.v_lds = lds + wave * kVTile;
@@ -770,7 +786,6 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     TileRegs r0, r1;
     fetch(d0, r0);
     fetch(d1, r1);
-    const QueryPart q = query_part(a, w, st, 0);
     const int q_scale = block_scale<DT>(q);
     const float down = scale_down(q_scale), mul = a.scale_log2e * scale_of((uint32_t)q_scale);
     unsigned char* const v_write = w.v_lds + li * kVRow + 64 * lg;
@@ -826,7 +841,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     }
     if (passed_over) with_table([&](const auto& t) __attribute__((always_inline)) { odd_tiles<DT, PAIRING, 1>(a, s, t, w, st); });
     with_table([&](const auto& t) __attribute__((always_inline)) {
-        if (holds<true>(t, w.t_begin, w.t_end, lane)) own_tiles<DT, PAIRING>(a, t, w, st);
+        if (holds<true>(t, w.t_begin, w.t_end, lane)) own_tiles<DT, PAIRING>(a, t, w, q, q_scale, st);
     });
     st.emit(w.massml, w.rows_wg, w.ss, false, li, lg);
 
@@ -888,6 +903,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), half = wave / kHalfWaves;
     const int li = lane & 15, lg = lane >> 4;
+    ask_for_arguments(a, p, s);
     // grid (split, kv head * row groups + row group, query)
     const int split = blockIdx.x, b = blockIdx.z;
     const int hkv = p.n_rg == 1 ? (int)blockIdx.y : (int)div_exact(blockIdx.y, (unsigned)p.n_rg), rg = (int)blockIdx.y - hkv * p.n_rg;
@@ -913,17 +929,21 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
         w.massml = a.mass ? reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * kRowsWg + wrow : nullptr;
         // the power of two that the workgroup's queries are scaled down by
         if (tid < 4) odd_lds[tid >> 1][tid & 1] = -1;
-        uint32_t top = 0;
         unsigned char* const q_lds = lds + kTiles + (wrow + li) * kQRow + 32 * lg;
+        QueryPart q[NRB];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) q[rb] = query_part(a, w.q_first, st, rb, lg);
+        __builtin_amdgcn_sched_barrier(0);
+        build_run_table(a, qh, &tbl, reinterpret_cast<SegTable*>(lds));
+        uint32_t top = 0;
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
-            const QueryPart q = query_part(a, w, st, rb);
-            top = max(top, largest<DT>(q));
+            top = max(top, largest<DT>(q[rb]));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = q.w[i];
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = q[rb].w[i];
         }
         reinterpret_cast<uint32_t*>(top_lds)[wave] = wave_top(top);
-        build_run_table(a, qh, &tbl, reinterpret_cast<SegTable*>(lds));              // (its barriers are after the lines above)
+        __syncthreads();
         const int total = wg_rows ? __builtin_amdgcn_readfirstlane(tbl.total) : 0;
         const int runs = HALVES ? 2 * p.nsplit : p.nsplit;
         w.t_begin = run_begin(total, runs, w.ss);
@@ -1056,6 +1076,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
             const int scale = own_scale<DT>(q_scale);
             const float own_down = scale_down(scale), own_mul = a.scale_log2e * scale_of((uint32_t)scale);
             const int pitch = a.n_kv_heads * kD * 2;
+            have_parts = false;
             for (;;) {
                 const Tile d = own.next(tbl, lane);
                 const bool any = d.ntok > 0;
@@ -1085,9 +1106,13 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                 const int t_end = HALVES ? half + (scalar(half ? e1.x : e0.x) > 0) : 1 + (scalar(e1.x) > 0);
 #pragma unroll 1
                 for (int t = HALVES ? half : 0; t < t_end; ++t) {
-                    const int ntok = scalar(t ? e1.x : e0.x), seg = scalar(t ? e1.y : e0.y), tok0 = scalar(t ? e1.w : e0.w);
+                    const int ntok = scalar(t ? e1.x : e0.x), seg = scalar(t ? e1.y : e0.y), delta = scalar(t ? e1.z : e0.z), tok0 = scalar(t ? e1.w : e0.w);
                     st.enter(seg, w.massml, kRowsWg, w.ss, false, li, lg);
-                    turn(std::integral_constant<int, DT>{}, t);
+                    if (!have_parts || delta != q_delta) {
+                        have_parts = true;
+                        q_delta = delta;
+                        turn(std::integral_constant<int, DT>{}, t);
+                    }
                     own_tile<DT, NRB>(st, qt, [&](int tb, int c) {
                         return *reinterpret_cast<const uint4*>(k_read + t * kKTile + 16 * tb * kKRow + 128 * (c >> 1) + 16 * (c & 1));
                     }, v_read + t * kVTile, tok0, ntok, own_mul, lg);
