@@ -28,7 +28,7 @@ RESOURCES = os.path.join(HERE, "kernel_resources.json")
 # kernels on the hot path that must keep everything in registers: a spill to scratch memory there
 # (a few lines of source can tip the register allocator over) costs far more than any tuning gains
 NO_SCRATCH = ("attn_tile_kernel", "attn_plain_kernel", "attn_wide_kernel", "attn_solo_kernel", "attn_combine_kernel", "plain_combine_kernel", "layer_epilogue_kernel",
-              "reposition_kernel", "assemble_kernel", "attn_q4_solo_kernel", "attn_q4_rows_kernel", "q4_combine_kernel", "q4_mass_kernel", "quantize_kernel")
+              "reposition_kernel", "assemble_kernel", "attn_q4_solo_kernel", "attn_q4_rows_kernel", "q4_merge_kernel", "quantize_kernel")
 
 
 def build(verbose: bool = True, jobs: int = 8) -> str:

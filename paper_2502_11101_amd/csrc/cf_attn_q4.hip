@@ -14,7 +14,7 @@
 // Work: the rows that share a kv head (row m = t * group + head) are cut into 16-row blocks.
 //   * One block (decode steps): attn_q4_solo_kernel, each of eight wavefronts streams a run of 32-token tiles of its own; they meet in LDS at the end.
 //   * More: attn_q4_rows_kernel, eight wavefronts that share the tiles that they stage together.
-// Splits (workgroups of the same rows) leave fp32 partial rows that q4_combine_kernel merges; q4_mass_kernel reduces the (reference, sum) pairs
+// Splits (workgroups of the same rows) leave fp32 partial rows that q4_merge_kernel merges; it also reduces the (reference, sum) pairs
 // that the wavefronts leave per row and segment where masses are wanted.
 #include "cf_attn_tile.h"
 #include "cf_plan_q4.h"
@@ -37,7 +37,8 @@ using attn::wave_lds_order;
 
 namespace {
 
-constexpr int kSoloThreads = kSoloWaves * kWave, kRowsThreads = kRowsWaves * kWave, kMassThreads = 1024;
+constexpr int kSoloThreads = kSoloWaves * kWave, kRowsThreads = kRowsWaves * kWave, kMergeThreads = 1024;
+constexpr int kMassRows = 2048;
 constexpr int kKRow = 272, kVRow = 288;              // bytes per token of a staged tile
 constexpr int kKTile = kTile * kKRow, kVTile = kTile * kVRow;
 constexpr int kRowBytes = 64;                        // codes of a row
@@ -1171,17 +1172,17 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
 }
 
 // ---------------------------------------------------------------------------------------------
-// Merges the splits' partial rows, a wavefront per row: lane s holds the statistics of split s, then a lane two channels.  A row's own
-// (maximum, sum) replaces split 0's, for the mass kernel.
+// What follows the attention: workgroups that work out masses (of one table entry each) and workgroups that merge the splits' partial rows, in one
+// launch, since they do not depend on each other.  Both are bound by latency.
+
+// Merges a row's partial rows, a wavefront per row: lane s holds the statistics of split s, then a lane two channels.
 template <int DT>
-__global__ __launch_bounds__(256) void q4_combine_kernel(AttnArgs a, Plan p) {
-    const int b = blockIdx.z, unit = b * p.units_per_b + (int)blockIdx.y;
-    const int hkv = p.n_rg == 1 ? (int)blockIdx.y : (int)div_exact(blockIdx.y, (unsigned)p.n_rg), rg = (int)blockIdx.y - hkv * p.n_rg;
-    const int lane = threadIdx.x & (kWave - 1);
-    const int row = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)threadIdx.x / kWave);
-    char* ws = static_cast<char*>(a.workspace);
+__device__ __forceinline__ void merge_row(const AttnArgs& a, const Plan& p, int b, int unit_of_b, int row, int lane) {
+    const int unit = b * p.units_per_b + unit_of_b;
+    const int hkv = p.n_rg == 1 ? unit_of_b : (int)div_exact((unsigned)unit_of_b, (unsigned)p.n_rg), rg = unit_of_b - hkv * p.n_rg;
+    const char* ws = static_cast<const char*>(a.workspace);
     const int64_t first = (int64_t)unit * p.nsplit * p.rows_wg + row;
-    float2* const ml = reinterpret_cast<float2*>(ws + p.off_ml) + first;
+    const float2* const ml = reinterpret_cast<const float2*>(ws + p.off_ml) + first;
     const float2* const opart = reinterpret_cast<const float2*>(ws + p.off_opart) + first * (kD / 2) + lane;
     const int q0 = a.q_off[b], q1 = a.q_off[b + 1];
     constexpr int kBatch = 8;
@@ -1196,7 +1197,7 @@ __global__ __launch_bounds__(256) void q4_combine_kernel(AttnArgs a, Plan p) {
     const float mx = wave_max(lane < p.nsplit ? stat.x : -INFINITY);
     const float m = mx == -INFINITY ? 0.f : mx;
     const float weight = lane < p.nsplit ? stat.y * __builtin_amdgcn_exp2f(stat.x - m) : 0.f;
-    const float l = wave_sum(weight);
+    const float l = wave_sum_dpp(weight);
     float2 o = make_float2(0.f, 0.f);
     for (int s0 = 0; s0 < p.nsplit; s0 += kBatch) {
         float2 x[kBatch];
@@ -1218,16 +1219,16 @@ __global__ __launch_bounds__(256) void q4_combine_kernel(AttnArgs a, Plan p) {
     const int t = (int)div_exact((unsigned)m2, (unsigned)p.group), g = m2 - t * p.group;
     uint32_t* op = static_cast<uint32_t*>(a.out) + (((int64_t)q0 + t) * a.n_q_heads + hkv * p.group + g) * (kD / 2) + lane;
     *op = Mma<DT>::pack(o.x * inv, o.y * inv);
-    if (a.mass && lane == 0) ml[0] = make_float2(mx, l);
 }
 
-// Per-segment attention mass, a workgroup per table entry: over the units, the runs that hold the segment's tiles and the rows, sum * exp2(reference -
-// row maximum) / row sum, in a fixed order.  Then S += mass (Alg. 2): a document slot's first entry works out the masses of all of the slot's
-// entries and adds them up in table order.  Bound by latency: the pairs of several items are asked for at once.
-__global__ __launch_bounds__(kMassThreads) void q4_mass_kernel(AttnArgs a, Plan p) {
+// Per-segment attention mass: over the units, the runs that hold the segment's tiles and the rows, sum * exp2(reference - row maximum) / row sum, in
+// a fixed order.  Then S += mass (Alg. 2): a document slot's first entry works out the masses of all of the slot's entries and adds them up in table
+// order.
+__device__ __forceinline__ void entry_mass(const AttnArgs& a, const Plan& p, int b, int entry) {
     __shared__ SegTable tbl;
-    __shared__ float part_sum[kMassThreads / kWave];
-    const int b = blockIdx.y, entry = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1);
+    __shared__ float part_sum[kMergeThreads / kWave];
+    __shared__ float2 stat[kMassRows];               // of the units at hand: row maximum, 1 / row sum
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const bool in_regs = a.seg_stride <= kWave;      // every wavefront keeps the table in registers
     const QueryHead qh = load_query_head(a, b, in_regs ? lane : tid);
     RegSegTable reg;
@@ -1239,48 +1240,79 @@ __global__ __launch_bounds__(kMassThreads) void q4_mass_kernel(AttnArgs a, Plan 
     const char* ws = static_cast<const char*>(a.workspace);
     const int tq = max(min(qh.tq_raw, a.max_tq), 0), n_rows = p.group * tq;
     const int nsub = p.nsplit * p.runs;
-    // items: unit, run, row; threads take rows of one (unit, run) side by side
-    const int rows = p.rows_wg <= 16 ? 16 : p.rows_wg <= 64 ? 64 : p.rows_wg <= 128 ? 128 : 256, per = (int)blockDim.x / rows;
-    const int row = tid & (rows - 1), first = tid / rows;
+    const int log_rows = p.rows_wg <= 16 ? 4 : p.rows_wg <= 64 ? 6 : p.rows_wg <= 128 ? 7 : 8, rows = 1 << log_rows;
+    const int row = tid & (rows - 1), first = tid >> log_rows, per = (int)blockDim.x >> log_rows;
+    const int chunk = kMassRows >> log_rows;         // units at a time
     const float inv_rg = 1.f / (float)p.n_rg, inv_nsub = 1.f / (float)nsub;
+    // whether `row` of unit u (of the query) is one of the query's (fewer than 2^21 units)
+    auto is_row = [&](int u) {
+        const int rg = p.n_rg == 1 ? 0 : u - (int)div_small((unsigned)u, (unsigned)p.n_rg, inv_rg) * p.n_rg;
+        return row < p.rows_wg && rg * p.rows_wg + row < n_rows;
+    };
+    constexpr int kBatch = 8;                        // loads in flight
     auto mass_of = [&](int s) {
         const int ts = in_regs ? __builtin_amdgcn_readlane(reg.t0, s) : tbl.tile0[s], te = in_regs ? __builtin_amdgcn_readlane(reg.t1, s) : tbl.tile0[s + 1];
         float sum = 0.f;
         if (te > ts) {
-            const int sub0 = run_of(total, nsub, ts), sub1 = run_of(total, nsub, te - 1);
-            const int n_sub = sub1 - sub0 + 1, items = p.units_per_b * n_sub;
-            const float2* const pairs = reinterpret_cast<const float2*>(ws + p.off_massml) + ((int64_t)b * p.units_per_b * p.slots + s + sub0) * p.rows_wg + row;
-            const float2* const whole = reinterpret_cast<const float2*>(ws + p.off_ml) + (int64_t)b * p.units_per_b * p.nsplit * p.rows_wg + row;
-            constexpr int kBatch = 8;
-            // item first + k * per as (unit, run), stepped without a division; fewer than 2^21 units
+            const int sub0 = run_of(total, nsub, ts), sub1 = run_of(total, nsub, te - 1), n_sub = sub1 - sub0 + 1;
             const float inv_sub = 1.f / (float)n_sub;
             const int du = (int)div_small((unsigned)per, (unsigned)n_sub, inv_sub), ds = per - du * n_sub;
-            int u = (int)div_small((unsigned)first, (unsigned)n_sub, inv_sub), sub = first - u * n_sub;
-            for (int left = items - first; left > 0; left -= kBatch * per) {
-                float2 v[kBatch], r[kBatch];
-                bool take[kBatch];
+            const int u_first = (int)div_small((unsigned)first, (unsigned)n_sub, inv_sub);
+            for (int u0 = 0; u0 < p.units_per_b; u0 += chunk) {
+                const int nu = min(chunk, p.units_per_b - u0);
+                const int64_t unit0 = (int64_t)b * p.units_per_b + u0;
+                const float2* const ml = reinterpret_cast<const float2*>(ws + p.off_ml) + unit0 * p.nsplit * p.rows_wg + row;
+                __syncthreads();                     // stat is free
+                for (int u = first; u < nu; u += per) {
+                    float m = -INFINITY, l = 0.f;
+                    if (!is_row(u0 + u)) {
+                    } else if (p.nsplit == 1) {
+                        const float2 v = ml[(int64_t)u * p.rows_wg];
+                        m = v.x;
+                        l = v.y;
+                    } else {
+                        for (int s0 = 0; s0 < p.nsplit; s0 += kBatch) {
+                            float2 v[kBatch];
+                            float top = m;
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j) {
-                    const int rg = p.n_rg == 1 ? 0 : u - (int)div_small((unsigned)u, (unsigned)p.n_rg, inv_rg) * p.n_rg;
-                    take[j] = j * per < left && row < p.rows_wg && rg * p.rows_wg + row < n_rows;
-                    // a run between a segment's first and last may own no tile at all: its slot was not written
-                    if (total < nsub) {
-                        const unsigned at = (unsigned)(total * (sub0 + sub));
-                        take[j] = take[j] && div_small(at, (unsigned)nsub, inv_nsub) < div_small(at + (unsigned)total, (unsigned)nsub, inv_nsub);
+                            for (int j = 0; j < kBatch; ++j) v[j] = ml[((int64_t)u * p.nsplit + min(s0 + j, p.nsplit - 1)) * p.rows_wg];
+#pragma unroll
+                            for (int j = 0; j < kBatch; ++j) top = fmaxf(top, v[j].x);
+                            const float safe = top == -INFINITY ? 0.f : top;
+                            l *= __builtin_amdgcn_exp2f(m - safe);
+#pragma unroll
+                            for (int j = 0; j < kBatch; ++j)
+                                if (s0 + j < p.nsplit) l += v[j].y * __builtin_amdgcn_exp2f(v[j].x - safe);
+                            m = top;
+                        }
                     }
-                    v[j] = r[j] = make_float2(0.f, 0.f);
-                    if (take[j]) {
-                        v[j] = pairs[((int64_t)u * p.slots + sub) * p.rows_wg];
-                        r[j] = whole[(int64_t)u * p.nsplit * p.rows_wg];
-                    }
-                    u += du;
-                    sub += ds;
-                    if (sub >= n_sub) { sub -= n_sub; ++u; }
+                    stat[(u << log_rows) + row] = make_float2(m == -INFINITY ? 0.f : m, l > 0.f ? 1.f / l : l);
                 }
+                __syncthreads();
+                // items: unit and run, item first + k * per stepped without a division; a group's threads take an item's rows side by side
+                const float2* const pairs = reinterpret_cast<const float2*>(ws + p.off_massml) + (unit0 * p.slots + s + sub0) * p.rows_wg + row;
+                int u = u_first, sub = first - u_first * n_sub;
+                for (int left = nu * n_sub - first; left > 0; left -= kBatch * per) {
+                    float2 v[kBatch], r[kBatch];
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j) {
-                    const float m = r[j].x == -INFINITY ? 0.f : r[j].x;
-                    if (take[j]) sum += v[j].y * __builtin_amdgcn_exp2f(v[j].x - m) * (r[j].y > 0.f ? 1.f / r[j].y : r[j].y);
+                    for (int j = 0; j < kBatch; ++j) {
+                        bool take = j * per < left && is_row(u0 + u);
+                        // a run between a segment's first and last may own no tile at all: its slot was not written
+                        if (total < nsub) {
+                            const unsigned at = (unsigned)(total * (sub0 + sub));
+                            take = take && div_small(at, (unsigned)nsub, inv_nsub) < div_small(at + (unsigned)total, (unsigned)nsub, inv_nsub);
+                        }
+                        v[j] = r[j] = make_float2(0.f, 0.f);
+                        if (take) {
+                            v[j] = pairs[((int64_t)u * p.slots + sub) * p.rows_wg];
+                            r[j] = stat[(u << log_rows) + row];
+                        }
+                        u += du;
+                        sub += ds;
+                        if (sub >= n_sub) { sub -= n_sub; ++u; }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kBatch; ++j) sum += v[j].y * __builtin_amdgcn_exp2f(v[j].x - r[j].x) * r[j].y;
                 }
             }
         }
@@ -1290,7 +1322,7 @@ __global__ __launch_bounds__(kMassThreads) void q4_mass_kernel(AttnArgs a, Plan 
         __syncthreads();
         float all = part_sum[0];
 #pragma unroll
-        for (int w = 1; w < kMassThreads / kWave; ++w)
+        for (int w = 1; w < kMergeThreads / kWave; ++w)
             if (w * kWave < (int)blockDim.x) all += part_sum[w];
         return all;
     };
@@ -1306,6 +1338,19 @@ __global__ __launch_bounds__(kMassThreads) void q4_mass_kernel(AttnArgs a, Plan 
         if (j > entry) sum += mass_of(j);
     }
     if (tid == 0) a.score_accum[(int64_t)b * a.score_stride + d] += sum;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kMergeThreads) void q4_merge_kernel(AttnArgs a, Plan p) {
+    // grid (table entries, then rows of all units; query)
+    const int b = blockIdx.y, entries = a.mass != nullptr ? a.seg_stride : 0;
+    if ((int)blockIdx.x < entries) {
+        entry_mass(a, p, b, blockIdx.x);
+        return;
+    }
+    const int row = __builtin_amdgcn_readfirstlane(((int)blockIdx.x - entries) * ((int)blockDim.x / kWave) + (int)threadIdx.x / kWave);
+    const int unit = (int)div_exact((unsigned)row, (unsigned)p.rows_wg);
+    if (unit < p.units_per_b) merge_row<DT>(a, p, b, unit, row - unit * p.rows_wg, threadIdx.x & (kWave - 1));
 }
 
 }  // namespace
@@ -1346,14 +1391,12 @@ cf_status launch_attention_q4(const AttnArgs& a, const q4::Scales& sc, const Rop
     if (bf16) by_pairing(std::integral_constant<int, CF_BF16>{});
     else by_pairing(std::integral_constant<int, CF_F16>{});
     CF_HIP(hipGetLastError());
-    if (!p.direct_out) {
-        const dim3 rows((unsigned)p.rows_wg / 4, (unsigned)p.units_per_b, (unsigned)a.batch);
-        if (bf16) hipLaunchKernelGGL(q4_combine_kernel<CF_BF16>, rows, dim3(256), 0, s, a, p);
-        else hipLaunchKernelGGL(q4_combine_kernel<CF_F16>, rows, dim3(256), 0, s, a, p);
-        CF_HIP(hipGetLastError());
-    }
-    if (a.mass != nullptr) {
-        hipLaunchKernelGGL(q4_mass_kernel, dim3((unsigned)a.seg_stride, (unsigned)a.batch), dim3((unsigned)p.mass_threads), 0, s, a, p);
+    const int64_t rows = p.direct_out ? 0 : (int64_t)p.units_per_b * p.rows_wg, per = p.merge_threads / kWave;
+    const int64_t blocks = (a.mass != nullptr ? a.seg_stride : 0) + (rows + per - 1) / per;
+    if (blocks > 0) {
+        const dim3 after((unsigned)blocks, (unsigned)a.batch);
+        if (bf16) hipLaunchKernelGGL(q4_merge_kernel<CF_BF16>, after, dim3((unsigned)p.merge_threads), 0, s, a, p);
+        else hipLaunchKernelGGL(q4_merge_kernel<CF_F16>, after, dim3((unsigned)p.merge_threads), 0, s, a, p);
         CF_HIP(hipGetLastError());
     }
     return CF_OK;

@@ -27,7 +27,7 @@ struct Plan {
     int rows_wg;        // rows a workgroup has room for
     int n_rg;           // row groups (workgroups side by side) per (query, kv head)
     int units_per_b, units, nsplit, slots;
-    int mass_threads;   // of a workgroup of q4_mass_kernel
+    int merge_threads;  // of a workgroup of q4_merge_kernel
     int direct_out;     // one split: the attention kernel writes the output rows itself
     size_t off_ml, off_opart, off_massml, total;
 };
@@ -63,7 +63,7 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({256 / std::max(p.units, 1), tiles / least, (int64_t)kMaxSplit}), 1);
     p.direct_out = p.nsplit == 1;
     // few table entries: many threads for each, whose loads are out at once; many: no more than have an item each
-    p.mass_threads = (int64_t)batch * seg_stride > 512 ? 256 : 1024;
+    p.merge_threads = (int64_t)batch * seg_stride > 512 ? 256 : 1024;
     p.slots = seg_stride + p.nsplit * p.runs;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
