@@ -1015,6 +1015,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
         for (int buf = 0;; buf ^= 1, ++step) {
             __syncthreads();                         // the step's tiles are staged; every wavefront is done with the other buffer
             const int4 e0 = desc_lds[buf][0], e1 = desc_lds[buf][1];
+            const int odd0 = odd_lds[buf][0], odd1 = odd_lds[buf][1];
             if (scalar(e0.x | e1.x) == 0) break;
             stage(dn, r, buf ^ 1, step + 1, false);
             fetch(dn, r);
@@ -1024,7 +1025,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                 const int slot = 2 * buf + t;
                 const int all = scalar(t ? e1.x : e0.x), seg = scalar(t ? e1.y : e0.y), delta = scalar(t ? e1.z : e0.z);
                 // a tile that is passed over counts as one without tokens (no branch around the body: the compiler would keep the accumulators twice)
-                const bool take = scalar(odd_lds[buf][t]) != step;
+                const bool take = scalar(t ? odd1 : odd0) != step;
                 const int ntok = take ? all : 0;
                 passed_over = passed_over || !take;
                 st.enter(seg, w.massml, kRowsWg, w.ss, false, li, lg);
@@ -1053,7 +1054,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                             sc[rb][tb] = Mma<CF_F16>::run(kf[c][tb], qt[rb].lo[c], sc[rb][tb]);
                             sc[rb][tb] = Mma<CF_F16>::run(kf[c][tb], qt[rb].hi[c], sc[rb][tb]);
                         }
-                __builtin_amdgcn_sched_barrier(0);
                 const Values vf = load_values(v_read + slot * kVTile);
                 __builtin_amdgcn_sched_barrier(0);
                 if (ntok < kTile) {

@@ -9,23 +9,38 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWavesHere = kThreads / kWave;
 
+// x / block_tokens for 0 <= x < 2^33: the estimate is off by at most one (a tenth of the instructions of a 64-bit division)
+struct Blocks {
+    int64_t tokens;
+    double per_token;
+    __device__ __forceinline__ explicit Blocks(int32_t block_tokens) : tokens(block_tokens), per_token(1.0 / block_tokens) {}
+    __device__ __forceinline__ int64_t of(int64_t x) const {
+        int64_t q = (int64_t)((double)x * per_token);
+        const int64_t r = x - q * tokens;
+        q += (r >= tokens ? 1 : 0) - (r < 0 ? 1 : 0);
+        return q;
+    }
+    __device__ __forceinline__ int64_t up(int64_t x) const { return of(x + tokens - 1); }
+};
+
 // What a request asks for.
 struct Ask {
     int64_t rows;       // new tokens
     int64_t want;       // blocks it needs beyond those it holds
     int64_t have;       // blocks it holds
     bool leaves, bad;   // gives its blocks back; its lengths do not fit its table
+    bool lost;          // not even what it holds is known
 };
-__device__ __forceinline__ Ask ask_of(const BlockArgs& a, int i) {
+__device__ __forceinline__ Ask ask_of(const BlockArgs& a, const Blocks& blocks, int i) {
     const int64_t cached = a.cached[i], fresh = a.fresh[i];
     Ask k;
     k.leaves = fresh < 0;
     k.rows = k.leaves ? 0 : fresh;
-    k.have = (max(cached, (int64_t)0) + a.block_tokens - 1) / a.block_tokens;
-    const int64_t need = (cached + k.rows + a.block_tokens - 1) / a.block_tokens;
+    k.have = blocks.up(max(cached, (int64_t)0));
+    const int64_t need = blocks.up(max(cached, (int64_t)0) + k.rows);
     k.bad = cached < 0 || k.have > a.table_stride || (!k.leaves && need > a.table_stride);
-    const bool lost = cached < 0 || k.have > a.table_stride;      // not even what it holds is known
-    if (lost) k.have = 0;
+    k.lost = cached < 0 || k.have > a.table_stride;
+    if (k.lost) k.have = 0;
     k.want = k.leaves || k.bad ? 0 : need - k.have;
     return k;
 }
@@ -66,6 +81,18 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* lds) {
     return v;
 }
 
+// how many threads up to this one, it included, have their flag set
+__device__ __forceinline__ int64_t block_count(bool flag, int64_t* lds) {
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const uint64_t all = __ballot(flag);
+    int64_t v = __popcll(all & (~0ull >> (kWave - 1 - lane)));
+    __syncthreads();
+    if (lane == 0) lds[wave] = __popcll(all);
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) v += lds[w];
+    return v;
+}
+
 // dynamic LDS: the request's blocks [table_stride], starts of its runs [table_stride + 1], and, where requests leave, how many blocks those up
 // to each give back [batch]
 __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
@@ -75,11 +102,12 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     int32_t* const starts = ids + a.table_stride;
     int32_t* const back_upto = starts + a.table_stride + 1;
     const int b = blockIdx.x, tid = threadIdx.x;
+    const Blocks blocks(a.block_tokens);
 
     // ---- the requests ahead of this one, and all of them
     int64_t t[5] = {0, 0, 0, 0, 0};                  // rows, wants, returns ahead; wants, returns of all
     for (int i = tid; i < a.batch; i += kThreads) {
-        const Ask k = ask_of(a, i);
+        const Ask k = ask_of(a, blocks, i);
         const int64_t back = k.leaves ? k.have : 0;
         if (i < b) { t[0] += k.rows; t[1] += k.want; t[2] += back; }
         t[3] += k.want;
@@ -87,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     }
     block_sums<5>(t, sums);
     const int64_t rows_before = t[0], want_before = t[1], back_before = t[2], back_all = t[4];
-    const Ask me = ask_of(a, b);
+    const Ask me = ask_of(a, blocks, b);
     const int64_t n_free_raw = a.n_free[0];
     const int64_t n_free = min(max(n_free_raw, (int64_t)0), (int64_t)a.n_blocks);
     const int64_t room = n_free + back_all;          // what the free list holds before anything is taken off it
@@ -98,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
         granted = 0;
         for (int i0 = 0; i0 < a.batch; i0 += kThreads) {
             const int i = i0 + tid;
-            const int64_t upto = carry + block_scan(i < a.batch ? ask_of(a, i).want : 0, scan);
+            const int64_t upto = carry + block_scan(i < a.batch ? ask_of(a, blocks, i).want : 0, scan);
             int64_t most[1] = {upto <= room ? upto : 0};
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) most[0] = max(most[0], (int64_t)__shfl_xor(most[0], o));
@@ -120,7 +148,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
             const int i = i0 + tid;
             int64_t mine = 0;
             if (i < a.batch) {
-                const Ask k = ask_of(a, i);
+                const Ask k = ask_of(a, blocks, i);
                 mine = k.leaves ? k.have : 0;
             }
             const int64_t upto = carry + block_scan(mine, scan);
@@ -158,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
         }
     __syncthreads();
     const int64_t cached = a.cached[b];
-    const bool lost = cached < 0 || (cached + a.block_tokens - 1) / a.block_tokens > a.table_stride;
+    const bool lost = me.lost;
     if (me.leaves)                                   // its blocks go on top of the free list, below what is handed on
         for (int j = tid; j < me.have; j += kThreads) {
             const int64_t at = n_free + back_before + j;
@@ -175,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
         if (at >= a.max_new_tokens) { too_many = true; break; }
         int64_t slot = -1;
         if (served) {
-            const int64_t tok = cached + r, j = tok / a.block_tokens;
+            const int64_t tok = cached + r, j = blocks.of(tok);
             const int32_t id = ids[j];
             if (id >= 0 && id < a.n_blocks) slot = a.first_token + (int64_t)id * a.block_tokens + (tok - j * a.block_tokens);
             else off_table = true;
@@ -198,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
         for (int64_t j0 = 0; j0 < me.have; j0 += kThreads) {
             const int64_t j = j0 + tid;
             const bool starts_run = j < me.have && (j == 0 || ids[j] != ids[j - 1] + 1);
-            const int64_t upto = carry + block_scan(starts_run ? 1 : 0, scan);
+            const int64_t upto = carry + block_count(starts_run, scan);
             if (starts_run) starts[upto - 1] = (int32_t)j;
             __syncthreads();
             if (tid == kThreads - 1) scan[0] = upto;
