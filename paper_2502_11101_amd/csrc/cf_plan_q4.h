@@ -38,7 +38,11 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     Plan p;
     p.group = n_q_heads / n_kv_heads;
     const int64_t blocks = ((int64_t)p.group * max_tq + 15) / 16;
+    // One block: a wavefront per run and no barriers (one row over 881 tokens x 32 heads 12.1 us, with rows_kernel and the merge that its
+    // splits then need 19.0; 32 rows over 1000 to 5000 tokens 25.4 and 69.2).
     p.solo = blocks <= 1;
+    // Up to four: four wavefronts hold all rows, and two such sets stream runs of their own (three blocks x 32 heads over 1680 tokens 27.2 us;
+    // with eight wavefronts' room for rows, half of it unused, 31.1: what is left unused costs the merge).
     p.halves = !p.solo && blocks <= 4;
     p.runs = p.solo ? kSoloWaves : p.halves ? 2 : 1;
     p.rows_wg = p.solo ? 16 : 64;
@@ -59,10 +63,14 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.units_per_b = n_kv_heads * p.n_rg;
     p.units = batch * p.units_per_b;
     const int64_t tiles = plan_tiles(seg_stride, max_kv_tokens);
+    // At most a workgroup per CU (registers leave no room for a second; 512 where one block streams: 32 conversations of 1000 to 5000 tokens 25.4
+    // -> 31.8 us, 4 of 24000 to 31000 23.0 -> 31.0), and no split below two tiles per wavefront, which the merge's launch would outweigh (one
+    // row over 881 tokens x 32 heads with one tile: 12.2 -> 14.8).
     const int64_t least = p.solo ? 2 * p.runs : 4;
     p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({256 / std::max(p.units, 1), tiles / least, (int64_t)kMaxSplit}), 1);
     p.direct_out = p.nsplit == 1;
-    // few table entries: many threads for each, whose loads are out at once; many: no more than have an item each
+    // Few table entries: many threads for each, whose loads are out at once (11 entries 8.2 us, with 256 threads 12.4; 52 10.7 and 17.0).  Many: no more
+    // threads than have work (64 queries of 21 entries 9.4 us, with 1024 threads 30.6).
     p.merge_threads = (int64_t)batch * seg_stride > 512 ? 256 : 1024;
     p.slots = seg_stride + p.nsplit * p.runs;
     size_t off = 0;
