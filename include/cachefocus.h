@@ -385,7 +385,7 @@ CF_API cf_status cf_prefill_layer(const cf_layer_desc* desc,
  *   codes   channel c in byte c / 2, even channels in its lower four bits.  Bit 3 is the sign, bits 0-2 the index of a
  *           magnitude in 0, 0.5, 1, 1.5, 2, 3, 4, 6.
  *   scales  byte g for channels 32g .. 32g + 31 stands for 2^(byte - 127); 255: every value of the group is NaN.
- * (The e2m1 and e8m0 formats of the OCP microscaling specification, which the matrix unit of gfx950 reads directly.)  Every value
+ * (The e2m1 and e8m0 formats of the OCP microscaling specification, which gfx950 has conversions for.)  Every value
  * that cf_quantize_cache writes is a number of the 16-bit type it was written from, so reading rounds nothing.
  * Layout: the descriptor's store strides, in elements (channels): a row's codes lie at (t * store_token_stride + h *
  * store_head_stride) / 2 bytes, its scales at a 32nd of that sum.  Both strides must be 0 or multiples of 128.
@@ -418,7 +418,7 @@ CF_API cf_status cf_quantize_cache(const cf_layer_desc* desc, const void* k, con
 /* ---------------------------------------------------------------------------------------------
  * cf_prefill_attention over a 4-bit store: the same mathematics, arguments and limits, with PREFIX and DOC entries read from `store`
  * (NULL: no entry lists store tokens) and the own block in 16 bits.  Decode steps are calls with max_tq = 1.
- * Stored keys and values enter as the numbers they stand for; the query, turned in fp32, enters with about 16 bits;
+ * Stored keys and values enter as the numbers they stand for; the query, turned in fp32, enters with 22 bits;
  * probabilities are rounded to 11 bits or more, sums and partial rows are fp32.
  * At most 256 table entries per query (CF_ERR_UNSUPPORTED beyond).  Own keys and values that are not finite reach only rows that see their
  * token.

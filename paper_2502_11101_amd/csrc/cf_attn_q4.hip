@@ -2,7 +2,7 @@
 //
 // A stored key or value row is 128 codes of four bits and four scale bytes (32 channels each).  What is moved to other positions is the query
 // and not the keys: (R_delta k) . q = k . (R_-delta q), once per segment instead of once per key (Eq. 5), and the keys stay exact.
-// Scores.  The turned query, scaled by a power of two, is split into two fp16 terms (22 bits); the keys, unpacked to fp16, are exact (at most two
+// Scores.  The turned query, scaled by a power of two of its row, is split into two fp16 terms (22 bits); the keys, unpacked to fp16, are exact (at most two
 // significant bits and an exponent inside fp16's), so that scores are right to fp32's accuracy on v_mfma_f32_16x16x32_f16.  (The scaled
 // 4-bit instruction, v_mfma_scale_f32_16x16x128_f8f6f4, takes the codes as they lie in memory against a query of e4m3 terms at the same matrix
 // cycles, but sums its 128 products with an error of up to 2^-13 of the largest one: attention masses were off by 2e-6 to 5e-6, and with an fp16 term
@@ -260,36 +260,31 @@ __device__ __forceinline__ uint32_t largest(const QueryPart& q) {
     }
     return top;
 }
-// The exponent byte of the power of two that queries are scaled down by: the largest channel, turned by any angle, comes to at most 2^7 * sqrt(2).
-template <int DT>
-__device__ __forceinline__ int scale_byte_of(uint32_t top) { return max((int)(__float_as_uint(Mma<DT>::lo(top)) >> 23) - 6, 27); }
+// The exponent byte of the power of two that a row of queries is scaled down by: its largest channel comes to between 1 and 2.
 template <int DT>
 __device__ __forceinline__ int row_scale(const QueryPart& q) {
     uint32_t top = largest<DT>(q);
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    return scale_byte_of<DT>(top);
+    return min(max((int)(__float_as_uint(Mma<DT>::lo(top)) >> 23), 27), 253);
 }
-
-// the largest over the 64 lanes
-__device__ __forceinline__ uint32_t wave_top(uint32_t v) {
-    auto step = [](uint32_t x, auto ctrl, auto rows) {
-        return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
-    };
-    using std::integral_constant;
-    v = step(v, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});     // row_shr:1, :2, :4, :8
-    v = step(v, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
-    v = step(v, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
-    v = step(v, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
-    v = step(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});     // row_bcast:15, :31
-    v = step(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, kWave - 1);
-}
-// the same for the block as a whole
-template <int DT>
-__device__ __forceinline__ int block_scale(const QueryPart& q) { return scale_byte_of<DT>(wave_top(largest<DT>(q))); }
-
+// The softmax scale (times log2 e) as a power of two, which multiplies scores, and a factor of the angles' cos and sin.  Scores times a power of two are
+// exact, so that the largest one less the reference made of it is zero whatever its size (times anything else it is off by a rounding of the
+// score, which exp2 of scores past 2^24 does not survive).
+__device__ __forceinline__ float scale_power(float scale_log2e) { return __uint_as_float(__float_as_uint(scale_log2e) & 0x7f800000u); }
+__device__ __forceinline__ float scale_factor(float scale_log2e) { return __uint_as_float((__float_as_uint(scale_log2e) & 0x807fffffu) | 0x3f800000u); }
 __device__ __forceinline__ float scale_down(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
+// The row in its own type, scaled: exact but for channels 2^-14 (fp16) of the largest and less, which keep what lies above 2^-25 of it.  (Every row by its
+// own: scaled together, a row with a channel 2^20 larger would take the bits of those beside it.)
+template <int DT>
+__device__ __forceinline__ QueryPart scaled(const QueryPart& q, int scale) {
+    const float down = scale_down(scale);
+    QueryPart r;
+    auto two = [&](uint32_t u) { return Mma<DT>::pack(Mma<DT>::lo(u) * down, Mma<DT>::hi(u) * down); };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = make_uint4(two(q.w[i].x), two(q.w[i].y), two(q.w[i].z), two(q.w[i].w));
+    return r;
+}
 
 // two floats as 16-bit values and what is left of them
 template <int DT>
@@ -536,11 +531,16 @@ struct WavePlace {
     float2* massml;             // slots of its rows, or NULL
 };
 
-// cos and sin of delta's 64 angles to LDS, times `down`
-__device__ __forceinline__ void put_angles(float2* cs, int lane, int delta, double my_freq, float down) {
+// cos and sin of an angle of the query's turn, with the softmax scale's factor
+__device__ __forceinline__ float2 turn_angle(const AttnArgs& a, int delta, double freq) {
+    const float2 c = rope_cos_sin_fast(delta, freq);
+    const float f = scale_factor(a.scale_log2e);
+    return make_float2(c.x * f, c.y * f);
+}
+// those of delta's 64 angles to LDS
+__device__ __forceinline__ void put_angles(const AttnArgs& a, float2* cs, int lane, int delta, double my_freq) {
     wave_lds_order();
-    const float2 c = rope_cos_sin_fast(delta, my_freq);
-    cs[lane] = make_float2(c.x * down, c.y * down);
+    cs[lane] = turn_angle(a, delta, my_freq);
     wave_lds_order();
 }
 
@@ -553,7 +553,7 @@ __device__ __forceinline__ QueryPart query_part(const AttnArgs& a, int64_t q_fir
 
 // The scale of a row of queries in the second pass, where keys have any scale: between its largest channel and 2^-9 there is room for keys
 // up to 2^127 and down to 2^-117.
-constexpr int kOddScale = 16;
+constexpr int kOddScale = 9;
 
 // The second pass over a run: the tiles whose scales do not fit fp16, in bf16: queries of three terms, probabilities as value and remainder.
 // The segments' slots hold sums already.
@@ -570,7 +570,7 @@ __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, co
         load_tile(a, s, d, walk.c_tok, w.hkv, w.li, w.lg, r);
         if (tile_fits(r, d.ntok, w.li, w.lg)) continue;
         st.enter(d.seg, w.massml, w.rows_wg, w.ss, true, w.li, w.lg);
-        put_angles(w.cs, lane, d.delta, w.my_freq, 1.f);
+        put_angles(a, w.cs, lane, d.delta, w.my_freq);
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
             uint4* const to = reinterpret_cast<uint4*>(w.v_lds + (16 * tb + w.li) * kVRow + 64 * w.lg);
@@ -617,12 +617,12 @@ __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, co
                 __builtin_amdgcn_sched_barrier(0);
             }
             const int lim = d.ntok - 4 * w.lg;
-            const float up = scale_of((uint32_t)scale);
+            const float up = scale_power(a.scale_log2e) * scale_of((uint32_t)scale);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] * up : -INFINITY;
         }
         float pv[NRB][8];
-        st.softmax(sc, [&](int) { return a.scale_log2e; }, pv);
+        st.softmax(sc, [&](int) { return 1.f; }, pv);
         st.template weigh<CF_BF16, true>(load_values(w.v_lds + (4 * w.lg + (w.li >> 2)) * kVRow + 8 * (w.li & 3)), pv);
         wave_lds_order();                            // the next tile writes over what others read above
     }
@@ -651,7 +651,7 @@ __device__ __forceinline__ void add_odd_values(__amdgpu_buffer_rsrc_t values, in
 
 // A tile of the own block: `ntok` keys (operands as in Parts, from key_at(tb, c)) and staged values; row t sees tokens 0 .. t.
 template <int DT, int NRB, class Key>
-__device__ __forceinline__ void own_tile(Rows<NRB>& st, const Parts (&qt)[NRB], Key key_at, const unsigned char* v_read, int tok0, int ntok, float mul, int lg) {
+__device__ __forceinline__ void own_tile(Rows<NRB>& st, const Parts (&qt)[NRB], Key key_at, const unsigned char* v_read, int tok0, int ntok, const float (&mul)[NRB], int lg) {
     f32x4 sc[NRB][2];
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) sc[rb][0] = sc[rb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -673,21 +673,15 @@ __device__ __forceinline__ void own_tile(Rows<NRB>& st, const Parts (&qt)[NRB], 
         for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) <= last ? sc[rb][e >> 2][e & 3] : -INFINITY;
     }
     float pv[NRB][8];
-    st.softmax(sc, [&](int) { return mul; }, pv);
+    st.softmax(sc, [&](int rb) { return mul[rb]; }, pv);
     st.template weigh<DT, true>(load_values(v_read), pv);
 }
 
-// The scale of the queries against own keys: fp16 has to hold them turned, bf16 does already (and its keys take up the whole range).
-template <int DT>
-__device__ __forceinline__ int own_scale(int scale) { return DT == CF_F16 ? scale : 127; }
-
 // The run's tiles of the own block, for a wavefront on its own.
 template <int DT, int PAIRING, class Table>
-__device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, const WavePlace& w, const QueryPart& q, int q_scale, Rows<1>& st) {
+__device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, const WavePlace& w, const QueryPart& q, float mul, Rows<1>& st) {
     const int lane = 16 * w.lg + w.li, li = w.li, lg = w.lg;
     RunWalk<true> walk(w.t_begin, w.t_end);
-    const int scale = own_scale<DT>(q_scale);
-    const float mul = a.scale_log2e * scale_of((uint32_t)scale);
     for (;;) {
         const Tile cd = walk.next(tbl, lane);
         if (cd.ntok <= 0) break;
@@ -704,7 +698,7 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, c
             }
         __builtin_amdgcn_sched_barrier(0);
         st.enter(cd.seg, w.massml, w.rows_wg, w.ss, false, li, lg);
-        put_angles(w.cs, lane, cd.delta, w.my_freq, scale_down(scale));
+        put_angles(a, w.cs, lane, cd.delta, w.my_freq);
         const Parts qt[1] = {to_parts<DT, PAIRING, DT>(q, w.cs, lg)};
         uint32_t odd = 0;                            // tokens with values that are not finite
 #pragma unroll
@@ -716,7 +710,7 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& a, const Table& tbl, c
             odd |= (uint32_t)((ballot | ballot >> 16 | ballot >> 32 | ballot >> 48) & 0xffff) << (16 * tb);
         }
         wave_lds_order();
-        own_tile<DT, 1>(st, qt, [&](int tb, int c) { return kf[tb][c]; }, w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3), cd.tok0, cd.ntok, mul, lg);
+        own_tile<DT, 1>(st, qt, [&](int tb, int c) { return kf[tb][c]; }, w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3), cd.tok0, cd.ntok, {mul}, lg);
         wave_lds_order();                            // the next tile writes over what others read above
         add_odd_values<DT, 1>(rv, pitch, odd, cd.tok0, lg, st);
     }
@@ -757,7 +751,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     Rows<1> st;
     st.begin(0, p.group * tq, p.group, a.n_q_heads, hkv, li);
     const int64_t q_first = (int64_t)qh.q0 * a.n_q_heads * kD;
-    const QueryPart q = query_part(a, q_first, st, 0, lg);           // (loads return in order: ahead of the tiles')
+    const QueryPart raw = query_part(a, q_first, st, 0, lg);         // (loads return in order: ahead of the tiles')
     RegSegTable rtbl;
     int total;
     if constexpr (REG_TABLE) {
@@ -792,8 +786,9 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     TileRegs r0, r1;
     fetch(d0, r0);
     fetch(d1, r1);
-    const int q_scale = block_scale<DT>(q);
-    const float down = scale_down(q_scale), mul = a.scale_log2e * scale_of((uint32_t)q_scale);
+    const int q_scale = row_scale<DT>(raw);
+    const QueryPart q = scaled<DT>(raw, q_scale);
+    const float mul = scale_power(a.scale_log2e) * scale_of((uint32_t)q_scale);
     unsigned char* const v_write = w.v_lds + li * kVRow + 64 * lg;
     const unsigned char* const v_read = w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
     Parts qt;
@@ -809,7 +804,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
         if (!have_parts || cd.delta != q_delta) {
             have_parts = true;
             q_delta = cd.delta;
-            put_angles(w.cs, lane, cd.delta, w.my_freq, down);
+            put_angles(a, w.cs, lane, cd.delta, w.my_freq);
             qt = to_parts<DT, PAIRING, CF_F16>(q, w.cs, lg);
         }
 #pragma unroll
@@ -847,7 +842,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     }
     if (passed_over) with_table([&](const auto& t) __attribute__((always_inline)) { odd_tiles<DT, PAIRING, 1>(a, s, t, w, st); });
     with_table([&](const auto& t) __attribute__((always_inline)) {
-        if (holds<true>(t, w.t_begin, w.t_end, lane)) own_tiles<DT, PAIRING>(a, t, w, q, q_scale, st);
+        if (holds<true>(t, w.t_begin, w.t_end, lane)) own_tiles<DT, PAIRING>(a, t, w, q, mul, st);
     });
     st.emit(w.massml, w.rows_wg, w.ss, false, li, lg);
 
@@ -907,7 +902,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
     __shared__ __attribute__((aligned(16))) float2 cs_lds[kRowsWaves][64];
     __shared__ __attribute__((aligned(16))) int4 desc_lds[2][2];     // tokens, segment, shift and first token of a staged tile
     __shared__ int odd_lds[2][2];                    // step of the last tile there whose scales do not fit fp16; own tiles: tokens with odd values
-    __shared__ __attribute__((aligned(16))) uint4 top_lds[kRowsWaves / 4];
     __shared__ float2 red_ml[HALVES ? kRowsWg : 1];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -937,7 +931,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
         w.cs = cs_lds[wave];
         w.v_lds = lds + wave * kVTile;
         w.massml = a.mass ? reinterpret_cast<float2*>(ws + p.off_massml) + (int64_t)unit * p.slots * kRowsWg + wrow : nullptr;
-        // the power of two that the workgroup's queries are scaled down by
         if (tid < 4) odd_lds[tid >> 1][tid & 1] = -1;
         unsigned char* const q_lds = lds + kTiles + (wrow + li) * kQRow + 32 * lg;
         QueryPart q[NRB];
@@ -945,14 +938,15 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
         for (int rb = 0; rb < NRB; ++rb) q[rb] = query_part(a, w.q_first, st, rb, lg);
         __builtin_amdgcn_sched_barrier(0);
         build_run_table(a, qh, &tbl, reinterpret_cast<SegTable*>(lds));
-        uint32_t top = 0;
+        float mul[NRB];
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
-            top = max(top, largest<DT>(q[rb]));
+            const int scale = row_scale<DT>(q[rb]);
+            mul[rb] = scale_power(a.scale_log2e) * scale_of((uint32_t)scale);
+            const QueryPart r = scaled<DT>(q[rb], scale);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = q[rb].w[i];
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = r.w[i];
         }
-        reinterpret_cast<uint32_t*>(top_lds)[wave] = wave_top(top);
         __syncthreads();
         const int total = wg_rows ? __builtin_amdgcn_readfirstlane(tbl.total) : 0;
         const int runs = HALVES ? 2 * p.nsplit : p.nsplit;
@@ -977,11 +971,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
             r.ks = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(s.k, at >> 5, scales), soff, 0, 0);
             r.vs = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(s.v, at >> 5, scales), soff, 0, 0);
         };
-        float down = 0.f;
-        auto angles = [&](int slot, int delta, float scale) __attribute__((always_inline)) {
-            const float2 c = rope_cos_sin_fast(delta, w.my_freq);
-            cs_lds[slot][lane] = make_float2(c.x * scale, c.y * scale);
-        };
+        auto angles = [&](int slot, int delta) __attribute__((always_inline)) { cs_lds[slot][lane] = turn_angle(a, delta, w.my_freq); };
         // tile d, loaded to r, to buffer `buf`; the first of a segment or run with its angles, which the half's wavefronts take turns in
         auto stage = [&](const Tile& d, const Regs& r, int buf, int step, bool first) __attribute__((always_inline)) {
             const bool fits = fits_f16(r.ks) && fits_f16(r.vs);
@@ -994,7 +984,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
             *reinterpret_cast<uint4*>(v_to + 16) = unpack8<CF_F16>(r.v.y, sv);
             if (!fits && st_tok < d.ntok) odd_lds[buf][half] = step;
             if ((tid & (kHalfThreads - 1)) == 0) desc_lds[buf][half] = make_int4(d.ntok, d.seg, d.delta, d.tok0);
-            if ((first || d.tok0 == 0) && ((wave ^ step) & (kHalfWaves - 1)) == 0) angles(2 * buf + half, d.delta, down);
+            if ((first || d.tok0 == 0) && ((wave ^ step) & (kHalfWaves - 1)) == 0) angles(2 * buf + half, d.delta);
         };
         auto scalar = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
         Parts qt[NRB];
@@ -1011,10 +1001,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
         Tile dn;
         Regs r;
         fetch(dn, r);
-        const uint4 t0 = top_lds[0], t1 = top_lds[1];
-        const int q_scale = scale_byte_of<DT>((uint32_t)scalar((int)max(max(max(t0.x, t0.y), max(t0.z, t0.w)), max(max(t1.x, t1.y), max(t1.z, t1.w)))));
-        down = scale_down(q_scale);
-        const float mul = a.scale_log2e * scale_of((uint32_t)q_scale);
         stage(dn, r, 0, 0, true);
         fetch(dn, r);
         int q_delta = 0, step = 0;
@@ -1073,7 +1059,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                         for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
                 }
                 float pv[NRB][8];
-                st.softmax(sc, [&](int) { return mul; }, pv);
+                st.softmax(sc, [&](int rb) { return mul[rb]; }, pv);
                 st.template weigh<CF_F16, false>(vf, pv);
             }
         }
@@ -1083,8 +1069,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
             // the own block, two tiles of 16-bit keys and values per step
             RunWalk<true> own(w.t_begin, w.t_end);
             if (!HALVES && half == 1) own.skip(tbl, lane);
-            const int scale = own_scale<DT>(q_scale);
-            const float own_down = scale_down(scale), own_mul = a.scale_log2e * scale_of((uint32_t)scale);
             const int pitch = a.n_kv_heads * kD * 2;
             have_parts = false;
             for (;;) {
@@ -1099,7 +1083,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                 const uint4 k1 = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, off + 16, 0, 0));
                 const uint4 v0 = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
                 const uint4 v1 = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rv, off + 16, 0, 0));
-                if ((wave & (kHalfWaves - 1)) == 0) angles(half, d.delta, own_down);
+                if ((wave & (kHalfWaves - 1)) == 0) angles(half, d.delta);
                 if ((tid & (kHalfThreads - 1)) == 0) { desc_lds[0][half] = make_int4(d.ntok, d.seg, d.delta, d.tok0); odd_lds[0][half] = 0; }
                 __syncthreads();
                 bool not_finite = false;
@@ -1125,7 +1109,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                     }
                     own_tile<DT, NRB>(st, qt, [&](int tb, int c) {
                         return *reinterpret_cast<const uint4*>(k_read + t * kKTile + 16 * tb * kKRow + 128 * (c >> 1) + 16 * (c & 1));
-                    }, v_read + t * kVTile, tok0, ntok, own_mul, lg);
+                    }, v_read + t * kVTile, tok0, ntok, mul, lg);
                     const uint32_t odd = (uint32_t)scalar(odd_lds[0][t]);
                     if (odd) {
                         const int64_t tok = scalar64(tbl.tok[seg]) + tok0;

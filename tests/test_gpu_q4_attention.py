@@ -195,6 +195,30 @@ def _small(hq=4, hkv=2, tq=6, n_store=200, dtype="bf16", seed=0):
     return host, t, upload(host, hkv, dtype, "head", "half", group=hq // hkv), {k: pl.to_device(v, dtype) for k, v in t.items()}
 
 
+@pytest.mark.parametrize("tq", [1, 20, 70, 200])
+@pytest.mark.parametrize("dtype,up", [("bf16", 40), ("f16", 13)])
+def test_a_row_far_larger_than_those_beside_it(dtype, up, tq):
+    """Its scale is its own: the rows that share its workgroup are as far off as they are without it, and it has finite values itself."""
+    host, t, s, dev = _small(tq=tq, dtype=dtype)
+    big = t["q"].copy()
+    big[0, 0] = wl.round_to_dtype(big[0, 0] * np.float32(2.0 ** up), dtype)
+    dev["q"] = pl.to_device(big, dtype)
+    rows = [(3, 150, 0, 40, cf.CF_SEG_DOC, 0), (20, 33, 0, 190, cf.CF_SEG_DOC, 1), (0, tq, 0, 300, cf.CF_SEG_SELF, -1)]
+    out = torch.empty_like(dev["q"])
+    _call(s, dev, [0, tq], [300], rows, [3], 3, 1, tq, 183 + tq, out)
+    torch.cuda.synchronize()
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    segs = [orc.Segment(o, n, a, p, k, d) for o, n, a, p, k, d in zip(*[[r[i] for r in rows] for i in range(4)],
+                                                                    [orc.KIND_DOC, orc.KIND_DOC, orc.KIND_SELF], [0, 1, -1])]
+    ks, vs = R.decode(host["k_codes"], host["k_scales"]), R.decode(host["v_codes"], host["v_scales"])
+    ck, cv, compact = H.compact_query(segs, ks, vs)
+    want, _, off, _ = R.attention(t["q"], 300, ck, cv, t["k_self"], t["v_self"], compact, 2, BASE)
+    ok = np.abs(got - want) <= R.HALF_STEP[dtype] * np.abs(want) + off + 1e-6 * np.abs(want).max()
+    ok[0, 0] = True
+    assert ok.all()
+
+
 def test_nan_stays_where_it_is_read():
     """A value group that is not a number reaches the channels it holds, a key row every channel, a query row its own output; rows past a
     list's end and tokens that are not listed reach nothing, nor do later tokens of the own block."""
