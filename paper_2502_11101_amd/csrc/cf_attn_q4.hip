@@ -1356,8 +1356,8 @@ size_t q4_workspace_bytes(const cf_layer_desc* d, int32_t batch, int32_t max_tq,
 cf_status launch_attention_q4(const AttnArgs& a, const q4::Scales& sc, const RopeFreq& f, hipStream_t s) {
     using namespace q4;
     const Plan p = make_plan(a.n_q_heads, a.n_kv_heads, a.batch, a.max_tq, a.seg_stride, a.max_kv_tokens);
-    if (a.batch > 65535 || p.units_per_b > 65535) {
-        set_error("neither batch nor n_kv_heads * row groups may exceed 65535 on this path");
+    if (a.batch > 65535 || p.units_per_b > 65535 || p.units == INT32_MAX) {
+        set_error("neither batch nor n_kv_heads * row groups may exceed 65535 on this path, nor both together 2^31 workgroups");
         return CF_ERR_UNSUPPORTED;
     }
     const dim3 grid((unsigned)p.nsplit, (unsigned)p.units_per_b, (unsigned)a.batch);

@@ -59,9 +59,12 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
             if (best == 0 || cost < best) { best = cost; p.rows_wg = rows; }
         }
     }
-    p.n_rg = (int)groups(p.rows_wg);
-    p.units_per_b = n_kv_heads * p.n_rg;
-    p.units = batch * p.units_per_b;
+    // (past what the launch takes these are bounds, and the call is refused)
+    constexpr int64_t kMost = INT32_MAX;
+    const int64_t units = std::min<int64_t>((int64_t)n_kv_heads * groups(p.rows_wg), kMost) * batch;
+    p.n_rg = (int)std::min(groups(p.rows_wg), kMost);
+    p.units_per_b = (int)std::min((int64_t)n_kv_heads * p.n_rg, kMost);
+    p.units = (int)std::min(units, kMost);
     const int64_t tiles = plan_tiles(seg_stride, max_kv_tokens);
     // At most a workgroup per CU (registers leave no room for a second; 512 where one block streams: 32 conversations of 1000 to 5000 tokens 25.4
     // -> 31.8 us, 4 of 24000 to 31000 23.0 -> 31.0), and no split below two tiles per wavefront, which the merge's launch would outweigh (one
@@ -75,10 +78,10 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.slots = seg_stride + p.nsplit * p.runs;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
-    const size_t rows = (size_t)p.units * p.nsplit * p.rows_wg;
+    const size_t rows = (size_t)units * p.nsplit * p.rows_wg;
     p.off_ml = take(rows * 2 * sizeof(float));
     p.off_opart = take(p.direct_out ? 0 : rows * kD * sizeof(float));
-    p.off_massml = take((size_t)p.units * p.slots * p.rows_wg * 2 * sizeof(float));
+    p.off_massml = take((size_t)units * p.slots * p.rows_wg * 2 * sizeof(float));
     p.total = off;
     return p;
 }

@@ -77,6 +77,7 @@ class BlockCache:
     layer ``attend`` and ``append`` with that layer's store.  Blocks are handed out of store tokens
     [first_token, first_token + n_blocks * block_tokens).  ``base_segs`` / ``n_base``: entries that lead a request's table (the shared
     prefix and documents); ``position``: position of its first own token.  Row t of a request's q / k / v carries RoPE for local position t.
+    A step swaps the arrays of lengths that it reads and writes: a program that records steps into graphs records two and replays them in turn.
     """
 
     def __init__(self, desc: cf.cf_layer_desc, batch: int, block_tokens: int, n_blocks: int, max_len: int, max_new: int,
@@ -101,6 +102,9 @@ class BlockCache:
         self.dev_flag = torch.zeros((1,), **i32)
         self.max_kv_tokens = max_base_tokens + max_len
         self.ws_bytes = cf.cf_prefill_workspace_bytes_q4(desc, batch, max_new, self.seg_stride, self.max_kv_tokens)
+        if self.ws_bytes == 0:
+            raise ValueError(f"a request's table of {self.seg_stride} entries (base_stride + blocks of max_len + 1), or the descriptor, is more than "
+                             "the attention over a 4-bit store serves: longer blocks, or a shorter max_len")
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
 
     def step(self, fresh) -> None:

@@ -195,6 +195,23 @@ def _small(hq=4, hkv=2, tq=6, n_store=200, dtype="bf16", seed=0):
     return host, t, upload(host, hkv, dtype, "head", "half", group=hq // hkv), {k: pl.to_device(v, dtype) for k, v in t.items()}
 
 
+# more workgroups than CUs: 192 rows per workgroup (two row blocks in one half's wavefronts, one in the other's), and 256
+@pytest.mark.parametrize("odd_scales", [False, True])
+@pytest.mark.parametrize("tq,dtype,pairing", [(32, "f16", "half"), (32, "bf16", "interleaved"), (42, "bf16", "half"), (42, "f16", "interleaved")])
+def test_many_queries_of_long_groups(tq, dtype, pairing, odd_scales):
+    rng = np.random.default_rng(tq)
+    batch = 70
+    tables = [docs(rng, int(rng.integers(0, 6)), 1, 90) for _ in range(batch)]
+    tables[0] = docs(rng, 7, 30, 90)
+
+    def change(host, t, rng):
+        odd = rng.random(host["v_codes"].shape[0]) < (0.05 if odd_scales else 0.0)
+        host["v_scales"] = np.where(odd[:, None, None], 127 - 24, host["v_scales"]).astype(np.uint8)
+        host["k_scales"] = np.where(odd[:, None, None], 127 - 25, host["k_scales"]).astype(np.uint8)
+    check(12, 2, tables, [tq] * (batch - 3) + [1, 0, 17], dtype=dtype, pairing=pairing, change=change, own_first=odd_scales,
+          compare=[0, 33, 67, 68, 69])
+
+
 @pytest.mark.parametrize("tq", [1, 20, 70, 200])
 @pytest.mark.parametrize("dtype,up", [("bf16", 40), ("f16", 13)])
 def test_a_row_far_larger_than_those_beside_it(dtype, up, tq):

@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 
 from paper_2502_11101_amd import binding as cf
+from paper_2502_11101_amd import pipeline as pl
 from tests import q4_reference as R
 
 FAKE = 0x10000      # never dereferenced: validation fails first
@@ -207,3 +208,17 @@ def test_a_step_of_blocks_by_hand():
     # a pool that runs short: the third request is not served, one that needs nothing is
     s = b.step([4, 0, 0, 6], [1, 4, 1, 1], np.zeros((4, 4), dtype=int) + 1, free, 2, [0] * 4)
     assert s["next_len"] == [5, 4, 0, 7] and s["flags"] == cf.CF_FLAG_NO_BLOCKS and s["slots"][5] == -1 and s["next_n_free"] == 0
+
+
+def test_block_cache_refuses_tables_that_the_attention_does_not_take():
+    s = pl.Q4Store(4, 2, "bf16", 1.0e4, 4096, 8, device="cpu")
+    with pytest.raises(ValueError, match="entries"):
+        pl.BlockCache(s.desc, 2, 16, 8, max_len=16 * 256, max_new=4, device="cpu")
+    assert pl.BlockCache(s.desc, 2, 16, 8, max_len=16 * 255, max_new=4, device="cpu").ws_bytes > 0
+
+
+def test_sizes_past_the_launch_are_no_small_workspace():
+    s = pl.Q4Store(64, 64, "bf16", 1.0e4, 4096, 8, device="cpu")
+    small = cf.cf_prefill_workspace_bytes_q4(s.desc, 1, 1 << 20, 4, 4096)
+    assert cf.cf_prefill_workspace_bytes_q4(s.desc, 1, (1 << 31) - 1, 4, 4096) > small
+    assert cf.cf_prefill_workspace_bytes_q4(s.desc, 65535, (1 << 24), 4, 4096) > small
