@@ -132,6 +132,9 @@ CASES = {
     "long": dict(hq=2, hkv=1, tables=[[(0, 6000, 0, 0)], [(100, 5900, 0, 0)]], lengths=[1, 1], n_store=6000),
     "long_rows": dict(hq=8, hkv=1, tables=[[(0, 3000, 0, 9), (3000, 2999, 0, 3)]], lengths=[9], n_store=6000),
     "bound_above_the_list": dict(hq=4, hkv=4, tables=[docs(RNG, 2, 9, 40)], lengths=[3], max_kv=100000, spare_entries=30),
+    # more rows over all heads than the masses' statistics have room for at a time
+    "many_heads": dict(hq=40, hkv=40, tables=[docs(RNG, 3, 10, 60)], lengths=[20]),
+    "many_heads_one_row": dict(hq=130, hkv=130, tables=[docs(RNG, 3, 10, 60)], lengths=[1], dtype="f16"),
 }
 
 
