@@ -378,3 +378,46 @@ def test_prefill_batch_prunes_by_the_masses_of_a_4_bit_store():
     torch.cuda.synchronize()
     assert pb.flags() == 0 and not torch.equal(first, out) and bool(torch.isfinite(out.float()).all())
     assert pb.mass[0, :5].sum().item() == pytest.approx(g.n_q_heads * cfg.tq, rel=1e-5)
+
+
+def test_calls_at_once_and_replays_of_a_recorded_pair():
+    """A decode step and a prefill on two streams at once, and both in a graph that is replayed, give what each gives alone."""
+    calls = []
+    for seed, tq in ((1, 1), (2, 70)):
+        host, t, s, dev = _small(tq=tq, seed=seed)
+        rows = [(3, 150, 0, 40, cf.CF_SEG_DOC, 0), (20, 120, 0, 190, cf.CF_SEG_DOC, 1), (0, tq, 0, 400, cf.CF_SEG_SELF, -1)]
+        need = cf.cf_prefill_workspace_bytes_q4(s.desc, 1, tq, 3, 270 + tq)
+        table, n_seg, q_off, q_pos = cf.segments_to_device(cf.segments_array(rows)), i32([3]), i32([0, tq]), i32([400])
+        ws, out, mass = torch.zeros(need, dtype=torch.uint8, device="cuda"), torch.zeros_like(dev["q"]), torch.zeros((1, 3), device="cuda")
+
+        def call(stream=None, s=s, dev=dev, tq=tq, need=need, table=table, n_seg=n_seg, q_off=q_off, q_pos=q_pos, ws=ws, out=out, mass=mass):
+            cf.cf_prefill_attention_q4(s.desc, dev["q"], q_off, 0, q_pos, s.store, dev["k_self"], dev["v_self"], table, n_seg, 3, 1, tq, 270 + tq,
+                                       out, mass, None, 1, ws, need, None, stream)
+        call()
+        torch.cuda.synchronize()
+        calls.append((call, out, mass, out.clone(), mass.clone()))
+
+    def same_and_clear():
+        torch.cuda.synchronize()
+        for _, out, mass, want, want_mass in calls:
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(mass, want_mass)
+            out.zero_()
+            mass.zero_()
+        torch.cuda.synchronize()
+    same_and_clear()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        for (call, *_), stream in zip(calls, streams):
+            call(stream)
+        same_and_clear()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            for call, *_ in calls:
+                call(side)
+    for _ in range(4):
+        graph.replay()
+        same_and_clear()
+        calls[1][0]()                                    # eager work between the replays
+        calls[0][0]()
+        same_and_clear()
