@@ -457,6 +457,11 @@ CF_API cf_status cf_assemble_cache_q4(const cf_layer_desc* desc, const cf_q4_sto
  *   base_segs, n_base, base_stride  device [batch*base_stride], [batch], or NULL: entries that lead each request's segment table
  *              (shared prefix and documents)
  *   q_stored_start  host: position that row 0 of a request's fresh q / k carries RoPE for
+ *   max_new_tokens  host: entries of slots and shift, and rows of the step's q, k, v and out
+ *   max_fresh  host: tokens that one request may add (max_tq of the step's attention calls), > 0: a request with more of them, or with rows
+ *              past max_new_tokens, is refused: it keeps its cached tokens and takes no block, its table is empty, its rows' slots are -1
+ *              (CF_FLAG_BAD_INDEX).  The rows of all requests lie back to back as `fresh` says, refused ones too; q_off ends at max_new_tokens.
+ *              0: no such check, for lengths that the caller knows to fit; where they do not, what is written must not be used.
  * Written:
  *   next_len   [batch] tokens held after the step, next_n_free [1], the free list's length after it (neither may alias its input)
  *   q_off      [batch+1], q_new_start [batch] = position + cached
@@ -468,13 +473,14 @@ CF_API cf_status cf_assemble_cache_q4(const cf_layer_desc* desc, const cf_q4_sto
  * its cached tokens, its fresh ones get slot -1 and next_len does not count them (CF_FLAG_NO_BLOCKS), though its rows still attend.
  * A request whose lengths do not fit its table is not served either (CF_FLAG_BAD_INDEX; with more cached tokens than the table
  * holds, or a negative number, its table is empty too), and bad block ids give slots of -1 and empty entries (CF_FLAG_BAD_INDEX).
- * More entries than seg_stride: n_seg = 0 and CF_FLAG_BAD_SEGMENT.  Fresh tokens past max_new_tokens: not written, CF_FLAG_BAD_INDEX. */
+ * More entries than seg_stride: n_seg = 0 and CF_FLAG_BAD_SEGMENT.  Without max_fresh, fresh tokens past max_new_tokens have no slot but
+ * count in every length, CF_FLAG_BAD_INDEX. */
 CF_API cf_status cf_block_tables(const int32_t* cached, const int32_t* fresh, int32_t batch, int32_t block_tokens, int32_t n_blocks,
                                  int64_t first_token, int32_t* table, int32_t table_stride, int32_t* free_blocks,
                                  const int32_t* n_free, const int32_t* position, const cf_segment* base_segs, const int32_t* n_base,
                                  int32_t base_stride, int32_t q_stored_start, int32_t* next_len, int32_t* next_n_free, int32_t* q_off,
-                                 int32_t* q_new_start, int64_t* slots, int32_t* shift, int64_t max_new_tokens, cf_segment* segs,
-                                 int32_t* n_seg, int32_t seg_stride, int32_t* dev_flag, void* stream);
+                                 int32_t* q_new_start, int64_t* slots, int32_t* shift, int64_t max_new_tokens, int32_t max_fresh,
+                                 cf_segment* segs, int32_t* n_seg, int32_t seg_stride, int32_t* dev_flag, void* stream);
 
 /* Thread-local text for the last non-OK status returned on this thread (static storage). */
 CF_API const char* cf_last_error(void);

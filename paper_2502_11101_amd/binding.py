@@ -137,8 +137,8 @@ def load() -> C.CDLL:
     lib.cf_assemble_cache_q4.restype = i32
     lib.cf_assemble_cache_q4.argtypes = [dp, sp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp]
     lib.cf_block_tables.restype = i32
-    lib.cf_block_tables.argtypes = [vp, vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp, vp,
-                                    i32, vp, vp]
+    lib.cf_block_tables.argtypes = [vp, vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i64, i32, vp,
+                                    vp, i32, vp, vp]
     _lib = lib
     return lib
 
@@ -360,10 +360,10 @@ def cf_assemble_cache_q4(desc, store: cf_q4_store, k_self, v_self, q_off, segs, 
 
 def cf_block_tables(cached, fresh, batch: int, block_tokens: int, n_blocks: int, first_token: int, table, table_stride: int, free_blocks,
                     n_free, position, base_segs, n_base, base_stride: int, q_stored_start: int, next_len, next_n_free, q_off, q_new_start,
-                    slots, shift, max_new_tokens: int, segs, n_seg, seg_stride: int, dev_flag=None, stream=None) -> None:
+                    slots, shift, max_new_tokens: int, segs, n_seg, seg_stride: int, dev_flag=None, stream=None, max_fresh: int = 0) -> None:
     status = (_native or _call()).block_tables(
         cached, fresh, batch, block_tokens, n_blocks, first_token, table, table_stride, free_blocks, n_free, position, base_segs, n_base,
-        base_stride, q_stored_start, next_len, next_n_free, q_off, q_new_start, slots, shift, max_new_tokens, segs, n_seg, seg_stride,
-        dev_flag, stream)
+        base_stride, q_stored_start, next_len, next_n_free, q_off, q_new_start, slots, shift, max_new_tokens, max_fresh, segs, n_seg,
+        seg_stride, dev_flag, stream)
     if status:
         _check(status)

@@ -589,14 +589,15 @@ cf_status cf_block_tables(const int32_t* cached, const int32_t* fresh, int32_t b
                           int64_t first_token, int32_t* table, int32_t table_stride, int32_t* free_blocks, const int32_t* n_free,
                           const int32_t* position, const cf_segment* base_segs, const int32_t* n_base, int32_t base_stride,
                           int32_t q_stored_start, int32_t* next_len, int32_t* next_n_free, int32_t* q_off, int32_t* q_new_start,
-                          int64_t* slots, int32_t* shift, int64_t max_new_tokens, cf_segment* segs, int32_t* n_seg, int32_t seg_stride,
-                          int32_t* dev_flag, void* stream) {
+                          int64_t* slots, int32_t* shift, int64_t max_new_tokens, int32_t max_fresh, cf_segment* segs, int32_t* n_seg,
+                          int32_t seg_stride, int32_t* dev_flag, void* stream) {
     CF_REQUIRE(batch >= 0, CF_ERR_INVALID_ARG, "batch is negative");
     CF_REQUIRE(batch <= kMaxBlockBatch, CF_ERR_UNSUPPORTED, "more than %d requests", kMaxBlockBatch);
     CF_REQUIRE(block_tokens >= 1 && n_blocks >= 0 && first_token >= 0, CF_ERR_INVALID_ARG,
                "need block_tokens >= 1, n_blocks >= 0 and first_token >= 0");
     CF_REQUIRE(table_stride >= 1 && seg_stride >= 1 && max_new_tokens >= 0, CF_ERR_INVALID_ARG,
                "need table_stride >= 1, seg_stride >= 1 and max_new_tokens >= 0");
+    CF_REQUIRE(max_fresh >= 0, CF_ERR_INVALID_ARG, "max_fresh is negative");
     CF_REQUIRE(table_stride <= kMaxBlockTable, CF_ERR_UNSUPPORTED, "more than %d blocks per request", kMaxBlockTable);
     CF_REQUIRE(q_stored_start >= 0, CF_ERR_RANGE, "q_stored_start is negative");
     CF_REQUIRE((base_segs == nullptr) == (n_base == nullptr) && (base_segs == nullptr || base_stride >= 1), CF_ERR_INVALID_ARG,
@@ -614,7 +615,7 @@ cf_status cf_block_tables(const int32_t* cached, const int32_t* fresh, int32_t b
     a.table = table; a.free_blocks = free_blocks; a.next_len = next_len; a.next_n_free = next_n_free; a.q_off = q_off;
     a.q_new_start = q_new_start; a.shift = shift; a.n_seg = n_seg; a.dev_flag = dev_flag; a.slots = slots; a.segs = segs;
     a.first_token = first_token; a.max_new_tokens = max_new_tokens; a.batch = batch; a.block_tokens = block_tokens; a.n_blocks = n_blocks;
-    a.table_stride = table_stride; a.base_stride = base_stride; a.q_stored_start = q_stored_start; a.seg_stride = seg_stride;
+    a.table_stride = table_stride; a.base_stride = base_stride; a.q_stored_start = q_stored_start; a.max_fresh = max_fresh; a.seg_stride = seg_stride;
     return launch_block_tables(a, static_cast<hipStream_t>(stream));
 }
 

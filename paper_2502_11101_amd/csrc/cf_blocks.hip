@@ -28,17 +28,20 @@ struct Ask {
     int64_t rows;       // new tokens
     int64_t want;       // blocks it needs beyond those it holds
     int64_t have;       // blocks it holds
-    bool leaves, bad;   // gives its blocks back; its lengths do not fit its table
+    bool leaves, bad;   // gives its blocks back; its lengths do not fit its table, or its rows the step
     bool lost;          // not even what it holds is known
+    bool over;          // more rows than a request may have, or than the step has room for
 };
-__device__ __forceinline__ Ask ask_of(const BlockArgs& a, const Blocks& blocks, int i) {
+// `fit`: the requests ahead of this one have room for all their rows.
+__device__ __forceinline__ Ask ask_of(const BlockArgs& a, const Blocks& blocks, int i, int fit) {
     const int64_t cached = a.cached[i], fresh = a.fresh[i];
     Ask k;
     k.leaves = fresh < 0;
     k.rows = k.leaves ? 0 : fresh;
     k.have = blocks.up(max(cached, (int64_t)0));
     const int64_t need = blocks.up(max(cached, (int64_t)0) + k.rows);
-    k.bad = cached < 0 || k.have > a.table_stride || (!k.leaves && need > a.table_stride);
+    k.over = k.rows > 0 && (i >= fit || (a.max_fresh > 0 && k.rows > a.max_fresh));
+    k.bad = cached < 0 || k.have > a.table_stride || (!k.leaves && need > a.table_stride) || k.over;
     k.lost = cached < 0 || k.have > a.table_stride;
     if (k.lost) k.have = 0;
     k.want = k.leaves || k.bad ? 0 : need - k.have;
@@ -97,7 +100,7 @@ __device__ __forceinline__ int64_t block_count(bool flag, int64_t* lds) {
 // to each give back [batch]
 __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     extern __shared__ int32_t smem[];
-    __shared__ int64_t sums[kWavesHere][5], scan[kWavesHere];
+    __shared__ int64_t sums[kWavesHere][6], scan[kWavesHere];
     int32_t* const ids = smem;
     int32_t* const starts = ids + a.table_stride;
     int32_t* const back_upto = starts + a.table_stride + 1;
@@ -105,17 +108,36 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     const Blocks blocks(a.block_tokens);
 
     // ---- the requests ahead of this one, and all of them
-    int64_t t[5] = {0, 0, 0, 0, 0};                  // rows, wants, returns ahead; wants, returns of all
-    for (int i = tid; i < a.batch; i += kThreads) {
-        const Ask k = ask_of(a, blocks, i);
-        const int64_t back = k.leaves ? k.have : 0;
-        if (i < b) { t[0] += k.rows; t[1] += k.want; t[2] += back; }
-        t[3] += k.want;
-        t[4] += back;
+    int64_t t[6];                                    // rows, wants, returns ahead; wants, returns, rows of all
+    auto tally = [&](int fit) {
+        for (int j = 0; j < 6; ++j) t[j] = 0;
+        for (int i = tid; i < a.batch; i += kThreads) {
+            const Ask k = ask_of(a, blocks, i, fit);
+            const int64_t back = k.leaves ? k.have : 0;
+            if (i < b) { t[0] += k.rows; t[1] += k.want; t[2] += back; }
+            t[3] += k.want;
+            t[4] += back;
+            t[5] += k.rows;
+        }
+        block_sums<6>(t, sums);
+    };
+    int fit = a.batch;
+    tally(fit);
+    if (a.max_fresh > 0 && t[5] > a.max_new_tokens) {                // workgroup-uniform: the requests up to the first whose rows run past the room
+        int64_t carry = 0;
+        fit = 0;
+        for (int i0 = 0; i0 < a.batch; i0 += kThreads) {
+            const int i = i0 + tid;
+            const int64_t upto = carry + block_scan(i < a.batch ? ask_of(a, blocks, i, a.batch).rows : 0, scan);
+            fit += __syncthreads_count(i < a.batch && upto <= a.max_new_tokens);
+            if (tid == kThreads - 1) scan[0] = upto;
+            __syncthreads();
+            carry = scan[0];
+        }
+        tally(fit);
     }
-    block_sums<5>(t, sums);
     const int64_t rows_before = t[0], want_before = t[1], back_before = t[2], back_all = t[4];
-    const Ask me = ask_of(a, blocks, b);
+    const Ask me = ask_of(a, blocks, b, fit);
     const int64_t n_free_raw = a.n_free[0];
     const int64_t n_free = min(max(n_free_raw, (int64_t)0), (int64_t)a.n_blocks);
     const int64_t room = n_free + back_all;          // what the free list holds before anything is taken off it
@@ -126,7 +148,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
         granted = 0;
         for (int i0 = 0; i0 < a.batch; i0 += kThreads) {
             const int i = i0 + tid;
-            const int64_t upto = carry + block_scan(i < a.batch ? ask_of(a, blocks, i).want : 0, scan);
+            const int64_t upto = carry + block_scan(i < a.batch ? ask_of(a, blocks, i, fit).want : 0, scan);
             int64_t most[1] = {upto <= room ? upto : 0};
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) most[0] = max(most[0], (int64_t)__shfl_xor(most[0], o));
@@ -148,7 +170,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
             const int i = i0 + tid;
             int64_t mine = 0;
             if (i < a.batch) {
-                const Ask k = ask_of(a, blocks, i);
+                const Ask k = ask_of(a, blocks, i, fit);
                 mine = k.leaves ? k.have : 0;
             }
             const int64_t upto = carry + block_scan(mine, scan);
@@ -215,13 +237,13 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     // ---- the segment table: shared entries, runs of neighbouring blocks, the own rows
     int n_base = 0;
     bool bad_base = false;
-    if (a.n_base && !me.leaves && !lost) {
+    if (a.n_base && !me.leaves && !lost && !me.over) {
         n_base = a.n_base[b];
         bad_base = n_base < 0 || n_base > a.base_stride;
         n_base = min(max(n_base, 0), a.base_stride);
     }
     int n_run = 0;
-    if (!me.leaves) {
+    if (!me.leaves && !me.over) {
         int64_t carry = 0;
         for (int64_t j0 = 0; j0 < me.have; j0 += kThreads) {
             const int64_t j = j0 + tid;
@@ -238,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
         if (tid == 0) starts[n_run] = (int32_t)me.have;
     }
     __syncthreads();
-    const bool own = me.rows > 0 && !lost;
+    const bool own = me.rows > 0 && !lost && !me.over;
     const int n = n_base + n_run + (own ? 1 : 0);
     const bool fits = n <= a.seg_stride;
     cf_segment* const out = a.segs + (int64_t)b * a.seg_stride;
@@ -278,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     a.n_seg[b] = fits ? n : 0;
     a.next_len[b] = me.leaves ? 0 : (int32_t)(served ? cached + me.rows : cached);
     a.q_new_start[b] = (int32_t)q_new;
-    const int64_t most = 0x7fffffff;
+    const int64_t most = a.max_fresh > 0 ? min(a.max_new_tokens, (int64_t)0x7fffffff) : 0x7fffffff;
     if (b == 0) { a.q_off[0] = 0; a.next_n_free[0] = (int32_t)min(left, (int64_t)a.n_blocks); }
     a.q_off[b + 1] = (int32_t)min(rows_before + me.rows, most);
     if (rows_before + me.rows > most) raise_flag(a.dev_flag, CF_FLAG_BAD_INDEX);

@@ -178,7 +178,7 @@ struct BlockArgs {
     int64_t* slots;
     cf_segment* segs;
     int64_t first_token, max_new_tokens;
-    int32_t batch, block_tokens, n_blocks, table_stride, base_stride, q_stored_start, seg_stride;
+    int32_t batch, block_tokens, n_blocks, table_stride, base_stride, q_stored_start, max_fresh, seg_stride;
 };
 constexpr int kMaxBlockBatch = 8192, kMaxBlockTable = 4095;      // what the kernel's LDS holds
 cf_status launch_block_tables(const BlockArgs& a, hipStream_t s);

@@ -219,19 +219,19 @@ CF_PY(assemble_cache_q4) {
 }
 
 CF_PY(block_tables) {
-    Args a(args, nargs, 27, "block_tables");
+    Args a(args, nargs, 28, "block_tables");
     void* cached = a.ptr(); void* fresh = a.ptr(); int32_t batch = a.i32(), block = a.i32(), n_blocks = a.i32(); int64_t first = a.i64();
     void* table = a.ptr(); int32_t table_stride = a.i32(); void* free_blocks = a.ptr(); void* n_free = a.ptr(); void* position = a.ptr();
     void* base = a.ptr(); void* n_base = a.ptr(); int32_t base_stride = a.i32(), q_stored = a.i32(); void* next_len = a.ptr();
     void* next_free = a.ptr(); void* q_off = a.ptr(); void* q_new = a.ptr(); void* slots = a.ptr(); void* shift = a.ptr();
-    int64_t max_new = a.i64(); void* segs = a.ptr(); void* n_seg = a.ptr(); int32_t seg_stride = a.i32(); void* flag = a.ptr();
+    int64_t max_new = a.i64(); int32_t max_fresh = a.i32(); void* segs = a.ptr(); void* n_seg = a.ptr(); int32_t seg_stride = a.i32(); void* flag = a.ptr();
     void* stream = a.stream();
     return finish(a, [&] {
         return cf_block_tables((const int32_t*)cached, (const int32_t*)fresh, batch, block, n_blocks, first, (int32_t*)table, table_stride,
                                (int32_t*)free_blocks, (const int32_t*)n_free, (const int32_t*)position, (const cf_segment*)base,
                                (const int32_t*)n_base, base_stride, q_stored, (int32_t*)next_len, (int32_t*)next_free, (int32_t*)q_off,
-                               (int32_t*)q_new, (int64_t*)slots, (int32_t*)shift, max_new, (cf_segment*)segs, (int32_t*)n_seg, seg_stride,
-                               (int32_t*)flag, stream);
+                               (int32_t*)q_new, (int64_t*)slots, (int32_t*)shift, max_new, max_fresh, (cf_segment*)segs, (int32_t*)n_seg,
+                               seg_stride, (int32_t*)flag, stream);
     });
 }
 

@@ -108,11 +108,13 @@ class BlockCache:
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)
 
     def step(self, fresh) -> None:
-        """The tables of a step in which the requests add `fresh` tokens; the rows of all requests lie back to back, in order."""
+        """The tables of a step in which the requests add `fresh` tokens, `max_new` each at the most; the rows of all requests lie back to back, in
+        order.  A request with more is refused: it keeps what it holds, its outputs are zero (past `max_new` rows: as they were), a bit of
+        `flags()` is set."""
         cf.cf_block_tables(self.len, fresh, self.batch, self.block_tokens, self.n_blocks, self.first_token, self.table, self.table_stride,
                            self.free_blocks, self.n_free, self.position, self.base_segs, self.n_base, self.base_stride, 0, self.next_len,
                            self.next_n_free, self.q_off, self.q_new, self.slots, self.shift, self.max_rows, self.segs, self.n_seg,
-                           self.seg_stride, self.dev_flag)
+                           self.seg_stride, self.dev_flag, None, self.max_new)
         self.len, self.next_len = self.next_len, self.len
         self.n_free, self.next_n_free = self.next_n_free, self.n_free
 
