@@ -67,7 +67,10 @@ class Q4Store:
     def write(self, k, v, slots, shift=None, dev_flag=None, n_live=None) -> None:
         """Rows of fresh keys and values to their slots, keys turned by `shift` positions (int32 per row) ahead of it; rows at and past
         `n_live` (device int32) are padding."""
-        cf.cf_quantize_cache(self.desc, k, v, int(k.shape[0]), slots, shift, self.store, dev_flag, None, n_live)
+        n = int(k.shape[0])
+        if v.shape[0] < n or slots.shape[0] < n or (shift is not None and shift.shape[0] < n):
+            raise ValueError(f"{n} keys, but fewer values, slots or shifts")
+        cf.cf_quantize_cache(self.desc, k, v, n, slots, shift, self.store, dev_flag, None, n_live)
 
 
 class BlockCache:
@@ -126,6 +129,8 @@ class BlockCache:
 
     def append(self, layer: Q4Store, k, v) -> None:
         """The step's keys, turned to their positions, and values go to their slots (k, v: the step's rows, and any padding behind them)."""
+        if k.shape[0] > self.max_rows:          # nothing but padding past the rows that a step has slots for
+            k, v = k[:self.max_rows], v[:self.max_rows]
         layer.write(k, v, self.slots, self.shift, self.dev_flag, self.q_off[self.batch:])
 
     def flags(self) -> int:
