@@ -10,7 +10,7 @@ from paper_2502_11101_amd import binding as cf
 from paper_2502_11101_amd import pipeline as pl
 from paper_2502_11101_amd import workloads as wl
 from tests import q4_reference as R
-from tests.test_gpu_q4_blocks import i32, pool
+from tests.test_gpu_q4_blocks import i32, pool, run_step
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,28 @@ def test_a_cache_goes_on_after_a_step_with_too_many_rows(fresh):
         assert cache.len.tolist() == lens
         assert cache.n_free.item() == n_blocks - sum(-(-x // block) for x in lens)
     assert refused_once
+
+
+def test_the_largest_step():
+    """8192 requests with room for 4095 blocks each: some hold all of them, some of those leave, and the newcomers take theirs."""
+    rng = np.random.default_rng(7)
+    B, stride, block = 8192, 4095, 2
+    cached = [int(x) for x in rng.integers(0, 7, size=B)]
+    fresh = [int(x) for x in rng.integers(0, 3, size=B)]
+    for b in (0, 1, 4000, 8190, 8191):
+        cached[b] = stride * block - b % 2               # full, or with room for one more token
+        fresh[b] = b % 2
+    for b in (1, 77, 300, 4000, 5000, 8191):
+        fresh[b] = -1
+    fresh[200] = 6000
+    have = [-(-c // block) for c in cached]
+    spare = 50                                           # far less than is taken: most comes from the requests that leave
+    first = np.concatenate([[0], np.cumsum(have)])
+    n_blocks = int(first[-1]) + spare
+    table = np.full((B, stride), -3)
+    for b in range(B):
+        table[b, :have[b]] = np.arange(first[b], first[b + 1])
+    free = np.full(n_blocks, -5)
+    free[:spare] = first[-1] + rng.permutation(spare)
+    want = run_step(R.Blocks(stride, block, n_blocks, 9, 3), cached, fresh, table, free, spare, [0] * B, use_position=False)
+    assert want["flags"] == 0 and want["next_n_free"] > 0
