@@ -7,7 +7,7 @@
 // 4-bit instruction, v_mfma_scale_f32_16x16x128_f8f6f4, takes the codes as they lie in memory against a query of e4m3 terms at the same matrix
 // cycles, but sums its 128 products with an error of up to 2^-13 of the largest one: attention masses were off by 2e-6 to 5e-6, and with an fp16 term
 // and one e4m3 term on that instruction by 7e-7 to 1.1e-6.)
-// Values are unpacked to fp16, staged in LDS and read transposed; probabilities are rounded to fp16 (2^-11), sums, maxima and accumulators
+// Values are unpacked to fp16, staged in LDS and read transposed; probabilities are rounded to fp16 (2^-11, see kLift), sums, maxima and accumulators
 // are fp32.  Tiles with a scale outside fp16's exponents are left to a second pass over the run, in bf16: queries of three terms,
 // probabilities as value and remainder.
 //
@@ -43,7 +43,18 @@ constexpr int kKRow = 272, kVRow = 288;              // bytes per token of a sta
 constexpr int kKTile = kTile * kKRow, kVTile = kTile * kVRow;
 constexpr int kRowBytes = 64;                        // codes of a row
 constexpr int kQRow = 272;                           // bytes per row of queries in LDS
-constexpr float kProbLimit = attn::kProbLimit;
+// Probabilities that are rounded to fp16 are relative to a reference kLift below a row's maximum in the exponent: the largest are 2^8, those down to 2^-22
+// of it keep eleven bits, those below a step of 2^-32 of it.  (Relative to the maximum itself: 2^-14 and 2^-24; of thousands of tokens 16 nats below a
+// dominant one 6 % were lost, from 17.5 nats on everything.)  The reference stays where it is until a lane's eight add up to more than
+// kLiftLimit, so that each is a number of fp16: room for 2^8 above it, as kProbLimit leaves without a lift.  (A lift of 11 with room for 2^5: 64 queries of
+// 384 rows x 2 heads 1.5 % slower, the reference moves more often.)
+constexpr int kLift = 8;
+constexpr float kLiftLimit = 65504.f;
+// Tiles in bf16 may have values of up to the type's largest, and bf16 probabilities any exponent: there the reference is kDrop above the maximum, so that
+// the accumulators, sums over thousands of tokens before they are divided, stay finite.
+constexpr int kDrop = -24;
+constexpr float kDropLimit = attn::kProbLimit / (1 << -kDrop);
+template <int DT> constexpr int kOwnLift = DT == CF_BF16 ? kDrop : kLift;
 
 // run i of a list of `total` tiles owns [total*i/n, total*(i+1)/n) (n at most 512, so that shorter lists need no 64-bit division)
 __device__ __forceinline__ int run_begin(int total, int n, int i) {
@@ -383,9 +394,10 @@ struct Rows {
 #pragma unroll
             for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(acc[rb][db]));
     }
-    // Online softmax (exp2 domain) of scores sc, in units of mul(block), against a stale row maximum: probabilities pv; see kProbLimit.
-    template <class F>
+    // Online softmax (exp2 domain) of scores sc, in units of mul(block), against a stale row maximum less LIFT: probabilities pv; see kLift.
+    template <int LIFT, class F>
     __device__ __forceinline__ void softmax(f32x4 (&sc)[NRB][2], F mul, float (&pv)[NRB][8]) {
+        constexpr float kLimit = LIFT > 0 ? kLiftLimit : kDropLimit;
         float lsum[NRB];
         auto probabilities = [&](int rb) __attribute__((always_inline)) {
             const float m_safe = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
@@ -400,7 +412,7 @@ struct Rows {
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
             probabilities(rb);
-            off = off || !(lsum[rb] <= kProbLimit) || m_run[rb] == -INFINITY;
+            off = off || !(lsum[rb] <= kLimit) || m_run[rb] == -INFINITY;
         }
         if (__any(off)) {
 #pragma unroll
@@ -411,6 +423,8 @@ struct Rows {
                 mloc *= mul(rb);                     // > 0: max commutes with it
                 mloc = fmaxf(mloc, __shfl_xor(mloc, 16));
                 mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
+                const float ref = mloc - LIFT;       // (a step of scores past 2^27 may come to more than the lift)
+                mloc = LIFT > 0 && mloc - ref > LIFT ? mloc : ref;
                 const float m_new = fmaxf(m_run[rb], mloc);
                 const float alpha = __builtin_amdgcn_exp2f(m_run[rb] - (m_new == -INFINITY ? 0.f : m_new));
 #pragma unroll
@@ -427,6 +441,19 @@ struct Rows {
             l_run[rb] += lsum[rb];
             seg_l[rb] += lsum[rb];
         }
+    }
+    // From kLift to kDrop.
+    __device__ __forceinline__ void lower() {
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            const float m_new = m_run[rb] + (kLift - kDrop), f = m_run[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - m_new);
+#pragma unroll
+            for (int db = 0; db < 8; ++db) acc[rb][db] *= f;
+            l_run[rb] *= f;
+            seg_l[rb] *= f;
+            m_run[rb] = m_new;
+        }
+        pin();
     }
     // O^T += V^T P^T, V of the type VT.  EXACT: P as value and remainder.
     template <int VT, bool EXACT>
@@ -622,7 +649,7 @@ __device__ __forceinline__ void odd_tiles(const AttnArgs& a, const Scales& s, co
             for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] * up : -INFINITY;
         }
         float pv[NRB][8];
-        st.softmax(sc, [&](int) { return 1.f; }, pv);
+        st.template softmax<kOwnLift<DT>>(sc, [&](int) { return 1.f; }, pv);
         st.template weigh<CF_BF16, true>(load_values(w.v_lds + (4 * w.lg + (w.li >> 2)) * kVRow + 8 * (w.li & 3)), pv);
         wave_lds_order();                            // the next tile writes over what others read above
     }
@@ -673,7 +700,7 @@ __device__ __forceinline__ void own_tile(Rows<NRB>& st, const Parts (&qt)[NRB], 
         for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) <= last ? sc[rb][e >> 2][e & 3] : -INFINITY;
     }
     float pv[NRB][8];
-    st.softmax(sc, [&](int rb) { return mul[rb]; }, pv);
+    st.template softmax<kOwnLift<DT>>(sc, [&](int rb) { return mul[rb]; }, pv);
     st.template weigh<DT, true>(load_values(v_read), pv);
 }
 
@@ -830,7 +857,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
             for (int e = 0; e < 8; ++e) sc[0][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[0][e >> 2][e & 3] : -INFINITY;
         }
         float pv[1][8];
-        st.softmax(sc, [&](int) { return mul; }, pv);
+        st.template softmax<kLift>(sc, [&](int) { return mul; }, pv);
         st.template weigh<CF_F16, false>(vf, pv);
         wave_lds_order();                            // the next step writes over what others read above
     };
@@ -840,9 +867,14 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
         if (d1.ntok <= 0) break;
         step(d1, r1);
     }
-    if (passed_over) with_table([&](const auto& t) __attribute__((always_inline)) { odd_tiles<DT, PAIRING, 1>(a, s, t, w, st); });
+    if (passed_over) {
+        if constexpr (DT == CF_BF16) st.lower();
+        with_table([&](const auto& t) __attribute__((always_inline)) { odd_tiles<DT, PAIRING, 1>(a, s, t, w, st); });
+    }
     with_table([&](const auto& t) __attribute__((always_inline)) {
-        if (holds<true>(t, w.t_begin, w.t_end, lane)) own_tiles<DT, PAIRING>(a, t, w, q, mul, st);
+        if (!holds<true>(t, w.t_begin, w.t_end, lane)) return;
+        if (DT == CF_BF16 && !passed_over) st.lower();
+        own_tiles<DT, PAIRING>(a, t, w, q, mul, st);
     });
     st.emit(w.massml, w.rows_wg, w.ss, false, li, lg);
 
@@ -1059,13 +1091,15 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
                         for (int e = 0; e < 8; ++e) sc[rb][e >> 2][e & 3] = 16 * (e >> 2) + (e & 3) < lim ? sc[rb][e >> 2][e & 3] : -INFINITY;
                 }
                 float pv[NRB][8];
-                st.softmax(sc, [&](int rb) { return mul[rb]; }, pv);
+                st.template softmax<kLift>(sc, [&](int rb) { return mul[rb]; }, pv);
                 st.template weigh<CF_F16, false>(vf, pv);
             }
         }
         const int wg_begin = HALVES ? run_begin(total, runs, 2 * split) : w.t_begin, wg_end = HALVES ? run_begin(total, runs, 2 * split + 2) : w.t_end;
         __syncthreads();                             // every wavefront is done with the tiles and their descriptions
-        if (holds<true>(tbl, wg_begin, wg_end, lane)) {
+        const bool own_tiles_here = holds<true>(tbl, wg_begin, wg_end, lane);
+        if (DT == CF_BF16 && (passed_over || own_tiles_here)) st.lower();
+        if (own_tiles_here) {
             // the own block, two tiles of 16-bit keys and values per step
             RunWalk<true> own(w.t_begin, w.t_end);
             if (!HALVES && half == 1) own.skip(tbl, lane);
