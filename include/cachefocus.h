@@ -418,8 +418,9 @@ CF_API cf_status cf_quantize_cache(const cf_layer_desc* desc, const void* k, con
 /* ---------------------------------------------------------------------------------------------
  * cf_prefill_attention over a 4-bit store: the same mathematics, arguments and limits, with PREFIX and DOC entries read from `store`
  * (NULL: no entry lists store tokens) and the own block in 16 bits.  Decode steps are calls with max_tq = 1.
- * Stored keys and values enter as the numbers they stand for; the query, turned in fp32, enters with 22 bits; probabilities are rounded to 11
- * bits or more, those below 2^-22 of a row's largest to multiples of 2^-32 of it; sums and partial rows are fp32.
+ * Stored keys and values enter as the numbers they stand for; the query, turned in fp32, enters with 22 bits (two terms of fp16; channels
+ * 2^-14 of a row's largest and less with fewer) and meets the own block's keys with two terms of desc->dtype (16 bits in bf16); probabilities
+ * are rounded to 11 bits or more, those below 2^-22 of a row's largest to multiples of 2^-32 of it; sums and partial rows are fp32.
  * At most 256 table entries per query (CF_ERR_UNSUPPORTED beyond).  Own keys and values that are not finite reach only rows that see their
  * token.
  * The workspace (cf_prefill_workspace_bytes_q4, 256-byte aligned) holds scratch only; one for some max_kv_tokens and seg_stride

@@ -676,7 +676,8 @@ __device__ __forceinline__ void add_odd_values(__amdgpu_buffer_rsrc_t values, in
     st.pin();
 }
 
-// A tile of the own block: `ntok` keys (operands as in Parts, from key_at(tb, c)) and staged values; row t sees tokens 0 .. t.
+// A tile of the own block: `ntok` keys (operands as in Parts, from key_at(tb, c)) and staged values; row t sees tokens 0 .. t.  Queries and
+// probabilities are two terms of the keys' type: 16 bits each in bf16, whose keys and values have eight.
 template <int DT, int NRB, class Key>
 __device__ __forceinline__ void own_tile(Rows<NRB>& st, const Parts (&qt)[NRB], Key key_at, const unsigned char* v_read, int tok0, int ntok, const float (&mul)[NRB], int lg) {
     f32x4 sc[NRB][2];
