@@ -284,6 +284,11 @@ __device__ __forceinline__ int row_scale(const QueryPart& q) {
 // score, which exp2 of scores past 2^24 does not survive).
 __device__ __forceinline__ float scale_power(float scale_log2e) { return __uint_as_float(__float_as_uint(scale_log2e) & 0x7f800000u); }
 __device__ __forceinline__ float scale_factor(float scale_log2e) { return __uint_as_float((__float_as_uint(scale_log2e) & 0x807fffffu) | 0x3f800000u); }
+// What a row's scores are in units of, from the exponent byte of its own power of two.  (Not zero, however small the softmax scale: a masked score is minus
+// infinity times this.)
+__device__ __forceinline__ float score_unit(float scale_log2e, int scale) {
+    return fmaxf(scale_power(scale_log2e) * __uint_as_float((uint32_t)scale << 23), 0x1p-126f);
+}
 __device__ __forceinline__ float scale_down(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
 // The row in its own type, scaled: exact but for channels 2^-14 (fp16) of the largest and less, which keep what lies above 2^-25 of it.  (Every row by its
 // own: scaled together, a row with a channel 2^20 larger would take the bits of those beside it.)
@@ -816,7 +821,7 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
     fetch(d1, r1);
     const int q_scale = row_scale<DT>(raw);
     const QueryPart q = scaled<DT>(raw, q_scale);
-    const float mul = scale_power(a.scale_log2e) * scale_of((uint32_t)q_scale);
+    const float mul = score_unit(a.scale_log2e, q_scale);
     unsigned char* const v_write = w.v_lds + li * kVRow + 64 * lg;
     const unsigned char* const v_read = w.v_lds + (4 * lg + (li >> 2)) * kVRow + 8 * (li & 3);
     Parts qt;
@@ -975,7 +980,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs 
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
             const int scale = row_scale<DT>(q[rb]);
-            mul[rb] = scale_power(a.scale_log2e) * scale_of((uint32_t)scale);
+            mul[rb] = score_unit(a.scale_log2e, scale);
             const QueryPart r = scaled<DT>(q[rb], scale);
 #pragma unroll
             for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(q_lds + rb * 16 * kQRow + 128 * (i >> 1) + 16 * (i & 1)) = r.w[i];

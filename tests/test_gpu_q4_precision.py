@@ -90,3 +90,23 @@ def test_values_near_the_largest_of_the_type(tq, heads, n):
             got, mass, segs = call(s, "bf16", q, 400, own, entries, heads)
             want, _, off, _ = Q.attention(q, 400, ks, vs, *(own or (None, None)), segs, heads, BASE)
             assert np.isfinite(got).all() and within(got, want, off, "bf16") <= 1
+
+
+@pytest.mark.parametrize("tq,heads", [(1, 2), (20, 2), (70, 2), (40, 130)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("scale", [1e-18, 1e-25, 1e-38])
+def test_softmax_scales_next_to_nothing(scale, dtype, tq, heads):
+    """Every token weighs the same, for rows of zeros and of tiny values as well, in tiles that are not full."""
+    rng = np.random.default_rng(tq)
+    n = 77
+    host = R.random_store(rng, n, heads, dtype)
+    s = upload(host, heads, dtype, "head", "half", scale)
+    ks, vs = R.decode(host["k_codes"], host["k_scales"]), R.decode(host["v_codes"], host["v_scales"])
+    normal = lambda m: wl.round_to_dtype(rng.standard_normal((m, heads, 128), dtype=np.float32), dtype)     # noqa: E731
+    q, own = normal(tq), (normal(tq), normal(tq))
+    q[0, 0] = 0
+    q[tq // 2, 1] = wl.round_to_dtype(q[tq // 2, 1] * np.float32(2.0 ** (-90 if dtype == "bf16" else -20)), dtype)
+    got, mass, segs = call(s, dtype, q, 400, own, [(0, n, 0, 0)], heads)
+    want, want_mass, off, mass_off = Q.attention(q, 400, ks, vs, *own, segs, heads, BASE, scale=scale, dtype=dtype)
+    assert within(got, want, off, dtype) <= 1
+    assert (np.abs(mass - want_mass) <= mass_off).all()
