@@ -386,7 +386,8 @@ CF_API cf_status cf_prefill_layer(const cf_layer_desc* desc,
  *           magnitude in 0, 0.5, 1, 1.5, 2, 3, 4, 6.
  *   scales  byte g for channels 32g .. 32g + 31 stands for 2^(byte - 127); 255: every value of the group is NaN.
  * (The e2m1 and e8m0 formats of the OCP microscaling specification, which gfx950 has conversions for.)  Every value
- * that cf_quantize_cache writes is a number of the 16-bit type it was written from, so reading rounds nothing.
+ * that cf_quantize_cache writes is a number of the 16-bit type it was written from, so reading rounds nothing.  (Of a
+ * store from elsewhere the gather rounds what is no number of desc->dtype, past its largest to infinities; attention takes numbers of bf16 as they are.)
  * Layout: the descriptor's store strides, in elements (channels): a row's codes lie at (t * store_token_stride + h *
  * store_head_stride) / 2 bytes, its scales at a 32nd of that sum.  Both strides must be 0 or multiples of 128.
  * The calls on such a store serve bf16 / fp16, head_dim 128, both pairings; others return CF_ERR_UNSUPPORTED. */
