@@ -75,8 +75,9 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a, Rope
     const int64_t slot = a.n_live && tok >= *a.n_live ? -1 : a.slots[tok];
     const int shift = a.shift ? a.shift[tok] : 0;
     if (a.shift) {
-        const int tok_last = (int)(min(row0 + kRows, n_rows) - 1) / a.n_kv_heads;
-        for (int i = tid; i < (tok_last - tok_first + 1) * kSlices; i += kThreads) {
+        // tokens of the workgroup's rows, from row numbers counted from its first token's (which 32 bits hold)
+        const int n_tok = (int)(min(row0 + kRows, n_rows) - 1 - (int64_t)tok_first * a.n_kv_heads) / a.n_kv_heads + 1;
+        for (int i = tid; i < n_tok * kSlices; i += kThreads) {
             const double x = (double)a.shift[tok_first + i / kSlices] * freq.rev[i % kSlices];
             double s, c;
             sincospi(2.0 * (x - rint(x)), &s, &c);
