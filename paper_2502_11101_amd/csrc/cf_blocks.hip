@@ -100,7 +100,7 @@ __device__ __forceinline__ int64_t block_count(bool flag, int64_t* lds) {
 // to each give back [batch]
 __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     extern __shared__ int32_t smem[];
-    __shared__ int64_t sums[kWavesHere][6], scan[kWavesHere];
+    __shared__ int64_t sums[kWavesHere][4], scan[kWavesHere];
     int32_t* const ids = smem;
     int32_t* const starts = ids + a.table_stride;
     int32_t* const back_upto = starts + a.table_stride + 1;
@@ -108,22 +108,22 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
     const Blocks blocks(a.block_tokens);
 
     // ---- the requests ahead of this one, and all of them
-    int64_t t[6];                                    // rows, wants, returns ahead; wants, returns, rows of all
+    // (wants and returns of all requests are less than 2^31, kMaxBlockBatch times kMaxBlockTable: two counts to a sum)
+    int64_t t[4];                                    // rows, wants and returns ahead; rows, wants and returns of all
     auto tally = [&](int fit) {
-        for (int j = 0; j < 6; ++j) t[j] = 0;
+        for (int j = 0; j < 4; ++j) t[j] = 0;
         for (int i = tid; i < a.batch; i += kThreads) {
             const Ask k = ask_of(a, blocks, i, fit);
-            const int64_t back = k.leaves ? k.have : 0;
-            if (i < b) { t[0] += k.rows; t[1] += k.want; t[2] += back; }
-            t[3] += k.want;
-            t[4] += back;
-            t[5] += k.rows;
+            const int64_t blocks_of = k.want | (k.leaves ? k.have : 0) << 32;
+            if (i < b) { t[0] += k.rows; t[1] += blocks_of; }
+            t[2] += k.rows;
+            t[3] += blocks_of;
         }
-        block_sums<6>(t, sums);
+        block_sums<4>(t, sums);
     };
     int fit = a.batch;
     tally(fit);
-    if (a.max_fresh > 0 && t[5] > a.max_new_tokens) {                // workgroup-uniform: the requests up to the first whose rows run past the room
+    if (a.max_fresh > 0 && t[2] > a.max_new_tokens) {                // workgroup-uniform: the requests up to the first whose rows run past the room
         int64_t carry = 0;
         fit = 0;
         for (int i0 = 0; i0 < a.batch; i0 += kThreads) {
@@ -136,13 +136,13 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(BlockArgs a) {
         }
         tally(fit);
     }
-    const int64_t rows_before = t[0], want_before = t[1], back_before = t[2], back_all = t[4];
+    const int64_t rows_before = t[0], want_before = (uint32_t)t[1], back_before = t[1] >> 32, back_all = t[3] >> 32;
     const Ask me = ask_of(a, blocks, b, fit);
     const int64_t n_free_raw = a.n_free[0];
     const int64_t n_free = min(max(n_free_raw, (int64_t)0), (int64_t)a.n_blocks);
     const int64_t room = n_free + back_all;          // what the free list holds before anything is taken off it
     // what is handed out: all of it, or where the list runs short the wants of the requests that still fit
-    int64_t granted = t[3];
+    int64_t granted = (uint32_t)t[3];
     if (granted > room) {
         int64_t carry = 0;
         granted = 0;
