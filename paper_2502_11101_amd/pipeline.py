@@ -185,7 +185,7 @@ class PrefillBatch:
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=device)   # contents are scratch
         self.n_alive = self.stride
         self.n_pending = 0          # layers whose scores are still pending in the workspace (layer(defer=True))
-        self._q4 = None             # workspace of attention_q4 and its size
+        self._q4 = {}               # workspaces of attention_q4 and their sizes, by the layer's heads (kept: a recorded graph may use them)
         self._cache = None          # device addresses and the prune-step structs of the current tables (layer())
 
     # -- Alg. 2 init: every document is a candidate, placement order = retriever order
@@ -208,12 +208,14 @@ class PrefillBatch:
 
     # -- the same over a store in 4 bits (whose descriptor replaces the batch's)
     def attention_q4(self, q, k_self, v_self, layer: Q4Store, out, accumulate: bool = True) -> None:
-        if self._q4 is None:
+        heads = layer.desc.n_q_heads, layer.desc.n_kv_heads
+        ws = self._q4.get(heads)
+        if ws is None:
             n = cf.cf_prefill_workspace_bytes_q4(layer.desc, self.batch, self.tq, self.seg_stride, self.max_kv_tokens)
-            self._q4 = (torch.zeros(n, dtype=torch.uint8, device=self.device), n)
+            ws = self._q4[heads] = (torch.zeros(n, dtype=torch.uint8, device=self.device), n)
         cf.cf_prefill_attention_q4(layer.desc, q, self.q_off, self.q_stored_start, self.q_start, layer.store, k_self, v_self, self.segs,
                                    self.n_seg, self.seg_stride, self.batch, self.tq, self.max_kv_tokens, out, self.mass,
-                                   self.score if accumulate else None, self.stride, *self._q4, self.dev_flag)
+                                   self.score if accumulate else None, self.stride, *ws, self.dev_flag)
 
     # -- Alg. 2: ids_sort = argsort(S); ids = prun(ids_sort); then Sec. 2.5 re-allocation.
     # Writes the next layer's tables; the current ones stay valid until advance().

@@ -1,5 +1,6 @@
 """Limits that the calls on a 4-bit cache store keep to, checked on the host: runs without a GPU."""
 
+import numpy as np
 import pytest
 import torch
 
@@ -46,3 +47,22 @@ def test_writes_with_fewer_slots_than_rows_are_refused(written):
     assert written == []
     s.write(_rows(4), _rows(5), slots, shift)            # more of them than rows: the rest is not used
     assert written == [(4, 4, 5, 5, 5)]
+
+
+@pytest.fixture
+def attended(monkeypatch):
+    """The arguments that cf_prefill_attention_q4 is called with, which is not called."""
+    calls = []
+    monkeypatch.setattr(cf, "cf_prefill_attention_q4", lambda *a, **k: calls.append(a))
+    return calls
+
+
+def test_a_batch_has_workspace_for_every_layer_it_is_given(attended):
+    layers = [pl.Q4Store(hq, hkv, "bf16", 1.0e4, 4096, 700, device="cpu") for hq, hkv in ((4, 4), (32, 32), (28, 4), (4, 4))]
+    lens = np.full((2, 5), 100)
+    pb = pl.PrefillBatch(layers[0].desc, np.arange(10).reshape(2, 5) * 100, lens, 48, 4, 4, 700, device="cpu")
+    for s in layers:
+        pb.attention_q4(None, None, None, s, None)
+        desc, seg_stride, batch, tq, kv, nbytes = (attended[-1][i] for i in (0, 10, 11, 12, 13, -2))
+        assert nbytes >= cf.cf_prefill_workspace_bytes_q4(desc, batch, tq, seg_stride, kv) > 0
+        assert attended[-1][-3].numel() >= nbytes
