@@ -39,7 +39,7 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.group = n_q_heads / n_kv_heads;
     const int64_t blocks = ((int64_t)p.group * max_tq + 15) / 16;
     // One block: a wavefront per run and no barriers (one row over 881 tokens x 32 heads 12.1 us, with rows_kernel and the merge that its
-    // splits then need 19.0; 32 rows over 1000 to 5000 tokens 25.4 and 69.2).
+    // splits then need 19.0; 32 conversations of 1000 to 5000 tokens 25.4 and 69.2).
     p.solo = blocks <= 1;
     // Up to four: four wavefronts hold all rows, and two such sets stream runs of their own (three blocks x 32 heads over 1680 tokens 27.2 us;
     // with eight wavefronts' room for rows, half of it unused, 31.1: what is left unused costs the merge).
@@ -73,8 +73,10 @@ inline Plan make_plan(int n_q_heads, int n_kv_heads, int batch, int max_tq, int 
     p.nsplit = (int)std::max<int64_t>(std::min<int64_t>({256 / std::max(p.units, 1), tiles / least, (int64_t)kMaxSplit}), 1);
     p.direct_out = p.nsplit == 1;
     // Few table entries: many threads for each, whose loads are out at once (11 entries 8.2 us, with 256 threads 12.4; 52 10.7 and 17.0).  Many: no more
-    // threads than have work (64 queries of 21 entries 9.4 us, with 1024 threads 30.6).
-    p.merge_threads = (int64_t)batch * seg_stride > 512 ? 256 : 1024;
+    // threads than have work (64 queries of 21 entries 9.4 us, with 1024 threads 30.6).  The lines cross between 102 and 164 entries (whole calls with 1024
+    // and 256 threads, 16 rows x 4 kv heads: 102 entries 27.4 and 27.8 us, 164 31.3 and 30.1, 336 43.5 and 38.5; 384 rows x 2: 31.2 and 34.2, 37.6 and
+    // 36.5, 61.4 and 55.2; 48 rows x 32: 47.5 and 51.0, 64.8 and 64.4, 118 and 116).
+    p.merge_threads = (int64_t)batch * seg_stride > 128 ? 256 : 1024;
     p.slots = seg_stride + p.nsplit * p.runs;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
