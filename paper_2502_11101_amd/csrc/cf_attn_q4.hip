@@ -759,8 +759,8 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t q_first, in
 // ---------------------------------------------------------------------------------------------
 // One row block (a decode step: one row per query head of a group): bound by HBM where there are enough tokens.  A wavefront's loads are two
 // tiles ahead in registers; a tile's codes meet the query in registers, its values pass through LDS of the wavefront's own.
-// Measured: 4 conversations of 24000 to 31000 tokens x 4 heads (60 MB) 18.4 us, in its loop 5.2 TB/s (a 2 GiB copy: 4.9), then 13 000 clocks of
-// prologue, merge of the wavefronts and the own tile; one row over 881 tokens x 32 heads 12.1 us, all of it such latency.  (The own tile ahead of
+// Measured: 4 conversations of 24000 to 31000 tokens x 4 heads (60 MB) 19.0 us, in its loop 5.2 TB/s (a 2 GiB copy: 4.9), then 13 000 clocks of
+// prologue, merge of the wavefronts and the own tile; one row over 881 tokens x 32 heads 12.1 us (12.6 in a trace), all of it such latency.  (The own tile ahead of
 // the loop, under the first tiles' loads: 0.4 us slower.)
 // REG_TABLE: the table in every wavefront's registers where it has at most 64 entries (12.1, 20.7 and 18.8 us for the two and 32 conversations of 1000
 // to 5000 tokens; from LDS 12.6, 21.8 and 19.5).
@@ -923,10 +923,10 @@ __global__ __launch_bounds__(kSoloThreads, 2) void attn_q4_solo_kernel(AttnArgs 
 //     second (a SIMD has a wavefront of either, so it gets NB0 + NB1).
 // A thread loads 8 bytes of a tile's key codes and of its value codes a step ahead of their staging, two ahead of their use, and unpacks them into
 // LDS, each once per workgroup, together with a description of the tile and the angles where a segment begins.  One barrier per step.
-// Measured: 64 queries of 384 rows x 2 heads over 3000 tokens in 20 segments 186 us (76 GFLOP that the method needs: 410 TFLOP/s; 1.5 times that runs,
+// Measured: 64 queries of 384 rows x 2 heads over 3000 tokens in 20 segments 179 us (76 GFLOP that the method needs: 425 TFLOP/s; 1.5 times that runs,
 // the scores being products of two terms): 6400 clocks per step of two wavefronts, of which the matrix pipe takes 2300 and the vector unit about
 // 3000, which add up to most of it; turning the queries is a quarter of the latter.  The halves' staging at opposite ends of a step, or a raised
-// priority for the products: no faster.  448 rows x 4 heads over 7500 tokens 34.8 us, 48 rows x 32 heads over 1680 19.1: half of it prologue and tail.
+// priority for the products: no faster.  448 rows x 4 heads over 7500 tokens 35.8 us, 48 rows x 32 heads over 1680 18.7: half of it prologue and tail.
 template <int DT, int PAIRING, int NB0, int NB1, bool HALVES>
 __global__ __launch_bounds__(kRowsThreads, 2) void attn_q4_rows_kernel(AttnArgs a, RopeFreq freq, Plan p, Scales s) {
     constexpr int kHalfWaves = kRowsWaves / 2, kHalfThreads = kRowsThreads / 2;

@@ -1,6 +1,6 @@
 // One scheduler step of a cache kept in blocks: from the requests' lengths the blocks they get and give back, the slots of their new tokens
 // and the segment tables and row offsets that the attention takes.  Integer work on a few KB per request, bound by latency: one
-// launch, a workgroup per request, each of which adds up the requests ahead of its own by itself (one request 4.9 us, 512 of them 10.0).
+// launch, a workgroup per request, each of which adds up the requests ahead of its own by itself (one request 4.7 us, 512 of them 9.7).
 #include "cf_common.h"
 
 namespace cf {

@@ -1,6 +1,6 @@
 // The writer of the cache store in 4 bits: fresh keys, turned to the position they are cached at (Eq. 5), and values go to their slots
 // as four-bit codes with a scale byte per 32 channels.  One pass, bound by HBM: 512 bytes of a key and a value row in, 136 out (4800 tokens of
-// 32 heads: 22.8 us = 4.4 TB/s, 89 % of what a 2 GiB copy reaches; 64 tokens of 4 heads 4.3 us, a launch's latency).
+// 32 heads: 23.4 us = 4.3 TB/s, 87 % of what a 2 GiB copy reaches; 64 tokens of 4 heads 4.3 us, a launch's latency).
 #include "cf_common.h"
 
 namespace cf {
