@@ -127,7 +127,7 @@ extern "C" {
 
 const char* cf_last_error(void) { return g_err; }
 
-int32_t cf_version(void) { return 100; }
+int32_t cf_version(void) { return 200; }      // 0.2: cf_block_tables takes max_fresh
 
 cf_status cf_profile_kernel_events(int32_t enable) {
     if (g_timer.on) {
