@@ -51,8 +51,9 @@ constexpr int kQRow = 272;                           // bytes per row of queries
 constexpr int kLift = 8;
 constexpr float kLiftLimit = 65504.f;
 // Tiles in bf16 may have values of up to the type's largest, and bf16 probabilities any exponent: there the reference is kDrop above the maximum, so that
-// the accumulators, sums over thousands of tokens before they are divided, stay finite.
-constexpr int kDrop = -24;
+// the accumulators, sums over thousands of tokens before they are divided, stay finite.  (No further above it: products of values next to nothing come
+// near fp32's smallest numbers; 2^-24 was more than values of 2^-112 bear.)
+constexpr int kDrop = -12;
 constexpr float kDropLimit = attn::kProbLimit / (1 << -kDrop);
 template <int DT> constexpr int kOwnLift = DT == CF_BF16 ? kDrop : kLift;
 

@@ -110,3 +110,19 @@ def test_softmax_scales_next_to_nothing(scale, dtype, tq, heads):
     want, want_mass, off, mass_off = Q.attention(q, 400, ks, vs, *own, segs, heads, BASE, scale=scale, dtype=dtype)
     assert within(got, want, off, dtype) <= 1
     assert (np.abs(mass - want_mass) <= mass_off).all()
+
+
+@pytest.mark.parametrize("tq,heads,n", [(1, 2, 300), (20, 2, 300), (70, 2, 300), (200, 130, 40)])
+def test_values_next_to_nothing(tq, heads, n):
+    """bf16 values of 2^-112 and less, in the store and in the own block: as near as any, relative to themselves."""
+    rng = np.random.default_rng(tq)
+    host = R.random_store(rng, n, heads, "bf16")
+    host["v_scales"][:] = 127 - 112
+    s = upload(host, heads, "bf16", "head", "half")
+    ks, vs = R.decode(host["k_codes"], host["k_scales"]), R.decode(host["v_codes"], host["v_scales"])
+    normal = lambda m: wl.round_to_dtype(rng.standard_normal((m, heads, 128), dtype=np.float32), "bf16")     # noqa: E731
+    k_self, v_self, q = normal(tq), normal(tq) * np.float32(2.0 ** -111), normal(tq)
+    for own in (None, (k_self, v_self)):
+        got, mass, segs = call(s, "bf16", q, 400, own, [(0, n, 0, 0)], heads)
+        want, _, off, _ = Q.attention(q, 400, ks, vs, *(own or (None, None)), segs, heads, BASE)
+        assert within(got, want, off, "bf16") <= 1
